@@ -434,6 +434,129 @@ repq_status repq_block_forward_host(const repq_block_desc* d, const repq_block_p
                                     const void* const* x_host, void* const* y_host, int n_batches,
                                     const repq_host_staging* s, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Serving: a decoder that answers token by token keeps the keys and values of what it has read in a paged cache
+ * of 8-bit codes, and says how probable tokens are.  (The paper evaluates its decoders by perplexity and zero-shot
+ * choice, Sec. IV-A, but describes neither a cache nor scoring; the quantizer is Eqs. 4-5 in its symmetric form.)
+ *
+ * The cache of one layer: num_blocks blocks of block_size tokens, for every block and key / value head one tile of
+ * block_size x d_h codes and one scale each for K and V,
+ *     value = scale[block, head] * (code - 128),   codes in 1..255   (Eq. 5 with z = 128).
+ * Token `slot` = block * block_size + offset.  A request's tokens lie in the blocks its row of the block table names,
+ * in order.  The caller owns the memory; a block needs no clearing before its first use.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct repq_cache {
+  uint8_t* k_codes;                     /* [device] [num_blocks][kv_heads][block_size][d_h], dense, 16-byte aligned */
+  uint8_t* v_codes;
+  float* k_scale;                       /* [device] [num_blocks][kv_heads] */
+  float* v_scale;
+  int32_t num_blocks, kv_heads;
+  int32_t block_size;                   /* 16, 32, 64 or 128 tokens */
+  int32_t d_h;                          /* a multiple of 16, at most 128 */
+} repq_cache;
+
+/* The plan of one step: request b holds kv_lens[b] tokens and brings q_lens[b] >= 0 more.  With old = ceil(kv / block_size) and
+ * new = ceil((kv + q) / block_size) blocks,
+ *     block_table[b, old .. new) = the next entries of free_list behind *free_head, requests in order;
+ *     kv_lens_out[b] = kv + q;   cu_q[b] = sum of q_lens before b, cu_q[requests] = their total;
+ *     positions[i] and slot_map[i] of token i of the step (tokens of a request in order, requests in order), -1 behind the last;
+ *     *free_head_out = *free_head + blocks taken;   totals = {tokens, blocks taken, blocks missing, longest kv_lens_out}.
+ * Other entries of the table are left alone.  Blocks that the list or the table's width does not hold are "missing": table entry
+ * and slots -1 (repq_cache_write skips such tokens, repq_cache_attention does not see them).  Outputs other than block_table may not
+ * be inputs (so the call can be repeated).  All pointers [device]; one kernel, nothing is read back. */
+typedef struct repq_cache_plan_desc {
+  int32_t requests, block_size;
+  int32_t table_width;                  /* entries of a table row that may be used */
+  int32_t free_blocks;                  /* entries of free_list */
+  int32_t slots;                        /* entries of slot_map and positions */
+  const int32_t* kv_lens;               /* int32[requests] */
+  const int32_t* q_lens;                /* int32[requests] */
+  int32_t* block_table;                 /* requests rows of ld_table entries */
+  int64_t ld_table;
+  const int32_t* free_list;
+  const int32_t* free_head;             /* int32[1] */
+  int32_t* kv_lens_out;                 /* int32[requests] */
+  int32_t* cu_q;                        /* int32[requests + 1] */
+  int32_t* slot_map;                    /* int32[slots] */
+  int32_t* positions;                   /* int32[slots] or NULL */
+  int32_t* free_head_out;               /* int32[1] */
+  int32_t* totals;                      /* int32[4] or NULL */
+} repq_cache_plan_desc;
+repq_status repq_cache_plan(const repq_cache_plan_desc* d, void* stream);
+
+/* Keys and values of `tokens` tokens into the cache.  For every (block, head) that gets rows, K and V apart,
+ *     a  = largest magnitude of the new rows,   s' = max(s if the block holds earlier rows, a * fl(1 / 127), 2^-60)
+ *     earlier codes: c' = round((c - 128) * (s / s')) + 128,    new codes: c = round(x / s') + 128
+ * round = half to even, float32 arithmetic, codes clipped to 1..255; the rows of a block in front of its first new row are its earlier
+ * rows.  A NaN is stored as zero, an infinity as the largest code.
+ * slot_map [device] int32[tokens]: slots below 0 or past the cache are skipped.  Tokens of one block must be neighbours with
+ * consecutive slots, as repq_cache_plan lays them out.  k, v [device]: REPQ_F32 or REPQ_BF16, token i, head h at
+ * base + i * stride_token + h * stride_head elements, d_h consecutive elements; rows 16-byte aligned. */
+typedef struct repq_cache_write_desc {
+  repq_cache cache;
+  int32_t tokens;
+  int32_t dtype;
+  const void* k;
+  int64_t k_stride_token, k_stride_head;
+  const void* v;
+  int64_t v_stride_token, v_stride_head;
+  const int32_t* slot_map;
+} repq_cache_write_desc;
+repq_status repq_cache_write(const repq_cache_write_desc* d, void* stream);
+
+/* Attention over the cache.  Request b has the queries [cu_q[b], cu_q[b + 1]) of the step, which are the last of its kv_lens[b] tokens:
+ *     S[i, j] = alpha q[i] . k[j],  j <= kv_lens[b] - q_len + i;    O[i] = sum_j softmax(S)[i, j] v[j]
+ * query head x reads key / value head x / (heads / kv_heads).  A row that sees no key gives 0 (lse -inf).  Table entries outside the
+ * cache hide their tokens.  Scores, sums and outputs are accumulated in float32; probabilities go into the product with 11
+ * significant bits for bf16 queries and with 22 for float32 ones (as do the queries).
+ * max_q_len, max_kv_len: bounds on the lengths of this step, from which the kernel and its grid are chosen; tokens past them are not
+ * computed (max_q_len) or not seen (max_kv_len).  Output as in repq_attention, row i, head x at out + i * ldo + x * o_stride_head; float
+ * outputs 16-byte, code outputs 4-byte aligned.  workspace: repq_cache_attention_workspace_bytes bytes (of the same descriptor), zero-filled before the first call that uses
+ * them; every call leaves them ready for the next (one at a time). */
+typedef struct repq_cache_attention_desc {
+  repq_cache cache;
+  int32_t requests, tokens, heads;
+  int32_t max_q_len, max_kv_len;
+  int32_t q_dtype;                      /* REPQ_F32 or REPQ_BF16 */
+  const void* q;                        /* [device] token i, head x at q + i * q_stride_token + x * q_stride_head, rows 16-byte aligned */
+  int64_t q_stride_token, q_stride_head;   /* elements */
+  const int32_t* block_table;           /* [device] requests rows of ld_table entries */
+  int64_t ld_table;
+  int32_t table_width;
+  const int32_t* kv_lens;               /* [device] int32[requests], this step's tokens included */
+  const int32_t* cu_q;                  /* [device] int32[requests + 1] */
+  float alpha;                          /* 1/sqrt(d_h) */
+  int32_t out_kind, out_bits;
+  float out_scale;
+  int32_t out_zero;
+  void* out;
+  int64_t ldo, o_stride_head;           /* elements (float kinds) or bytes (codes) */
+  int32_t* out_row_sum;                 /* [device] int32[tokens] or NULL: with REPQ_OUT_CODES the row sums are ADDED here */
+  float* lse;                           /* [device] float[tokens * heads] or NULL: ln sum_j exp(S[i, j]) */
+} repq_cache_attention_desc;
+repq_status repq_cache_attention_workspace_bytes(const repq_cache_attention_desc* d, size_t* bytes);
+repq_status repq_cache_attention(const repq_cache_attention_desc* d, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Log probabilities of given tokens.  Per row of logits x (row stride ld elements), with m = max x and Z = sum exp(x - m):
+ *     logprob = x[t] - m - ln Z;    entropy = ln Z - sum exp(x - m) (x - m) / Z      (nats; terms of x = -inf are 0)
+ *     rank    = 1 + number of tokens before t in the order (logit descending, index ascending)
+ *     top_ids, top_logprobs: the first `top` tokens of that order, dense rows of `top` entries
+ * A token outside 0..vocab-1 (padding) gives logprob 0 and rank 0.  A row of -inf alone gives logprobs -inf, entropy 0; a NaN or +inf in a row makes its
+ * float outputs NaN (NaN comes last in the order).  tokens may be NULL if logprob and rank are.  All pointers [device]. */
+typedef struct repq_token_logprobs_desc {
+  int32_t rows, vocab, top;             /* 0 <= top <= min(vocab, 32) */
+  int32_t dtype;                        /* REPQ_F32 or REPQ_BF16 */
+  const void* logits;
+  int64_t ld;
+  const int32_t* tokens;                /* int32[rows] */
+  float* logprob;                       /* float[rows] or NULL */
+  float* entropy;                       /* float[rows] or NULL */
+  int32_t* rank;                        /* int32[rows] or NULL */
+  int32_t* top_ids;                     /* int32[rows * top] (NULL if top is 0) */
+  float* top_logprobs;                  /* float[rows * top] */
+} repq_token_logprobs_desc;
+repq_status repq_token_logprobs(const repq_token_logprobs_desc* d, void* stream);
+
 /* Number of CUDA kernels this library has launched in the calling process so far. */
 uint64_t repq_launch_count(void);
 

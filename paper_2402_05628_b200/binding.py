@@ -7,7 +7,8 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional, Sequence
+import struct
+from typing import NamedTuple, Optional, Sequence
 
 import numpy as np
 import torch
@@ -31,6 +32,7 @@ EXPORTS = (
     "repq_device_status", "repq_block_forward_timed", "repq_launch_count",
     "repq_block_forward_static", "repq_attention", "repq_block_forward_host", "repq_rope_table",
     "repq_bounded_wait_selftest", "repq_dual_clip", "repq_layernorm",
+    "repq_cache_plan", "repq_cache_write", "repq_cache_attention_workspace_bytes", "repq_cache_attention", "repq_token_logprobs",
 )
 REPQ_MLP_GELU, REPQ_MLP_SWIGLU = 0, 1
 REPQ_STATIC_WORKSPACE_BYTES = 8 << 20
@@ -125,6 +127,42 @@ class BlockParams(C.Structure):
     ]
 
 
+class CacheDesc(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("num_blocks", C.c_int32), ("kv_heads", C.c_int32), ("block_size", C.c_int32), ("d_h", C.c_int32)]
+
+
+class CachePlanDesc(C.Structure):
+    _fields_ = [("requests", C.c_int32), ("block_size", C.c_int32), ("table_width", C.c_int32), ("free_blocks", C.c_int32),
+                ("slots", C.c_int32), ("kv_lens", C.c_void_p), ("q_lens", C.c_void_p), ("block_table", C.c_void_p),
+                ("ld_table", C.c_int64), ("free_list", C.c_void_p), ("free_head", C.c_void_p), ("kv_lens_out", C.c_void_p),
+                ("cu_q", C.c_void_p), ("slot_map", C.c_void_p), ("positions", C.c_void_p), ("free_head_out", C.c_void_p),
+                ("totals", C.c_void_p)]
+
+
+class CacheWriteDesc(C.Structure):
+    _fields_ = [("cache", CacheDesc), ("tokens", C.c_int32), ("dtype", C.c_int32),
+                ("k", C.c_void_p), ("k_stride_token", C.c_int64), ("k_stride_head", C.c_int64),
+                ("v", C.c_void_p), ("v_stride_token", C.c_int64), ("v_stride_head", C.c_int64), ("slot_map", C.c_void_p)]
+
+
+class CacheAttentionDesc(C.Structure):
+    _fields_ = [("cache", CacheDesc), ("requests", C.c_int32), ("tokens", C.c_int32), ("heads", C.c_int32),
+                ("max_q_len", C.c_int32), ("max_kv_len", C.c_int32), ("q_dtype", C.c_int32),
+                ("q", C.c_void_p), ("q_stride_token", C.c_int64), ("q_stride_head", C.c_int64),
+                ("block_table", C.c_void_p), ("ld_table", C.c_int64), ("table_width", C.c_int32),
+                ("kv_lens", C.c_void_p), ("cu_q", C.c_void_p), ("alpha", C.c_float),
+                ("out_kind", C.c_int32), ("out_bits", C.c_int32), ("out_scale", C.c_float), ("out_zero", C.c_int32),
+                ("out", C.c_void_p), ("ldo", C.c_int64), ("o_stride_head", C.c_int64),
+                ("out_row_sum", C.c_void_p), ("lse", C.c_void_p)]
+
+
+class TokenLogprobsDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("vocab", C.c_int32), ("top", C.c_int32), ("dtype", C.c_int32),
+                ("logits", C.c_void_p), ("ld", C.c_int64), ("tokens", C.c_void_p), ("logprob", C.c_void_p),
+                ("entropy", C.c_void_p), ("rank", C.c_void_p), ("top_ids", C.c_void_p), ("top_logprobs", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -169,6 +207,11 @@ def lib() -> C.CDLL:
         _lib.repq_dual_clip.argtypes = [C.c_void_p, C.c_int64, C.c_int, C.c_int64, C.c_int, C.c_int, C.c_float, C.c_float,
                                         C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
         _lib.repq_bounded_wait_selftest.argtypes = [C.c_int64, C.c_void_p]
+        _lib.repq_cache_plan.argtypes = [C.c_void_p, C.c_void_p]
+        _lib.repq_cache_write.argtypes = [C.c_void_p, C.c_void_p]
+        _lib.repq_cache_attention_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
+        _lib.repq_cache_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        _lib.repq_token_logprobs.argtypes = [C.c_void_p, C.c_void_p]
     return _lib
 
 
@@ -390,6 +433,151 @@ def repq_rope_table(seq: int, d_h: int, base: float = 10000.0) -> np.ndarray:
     t = np.empty((seq, d_h // 2, 2), dtype=np.float32)
     _check(lib().repq_rope_table(seq, d_h, float(base), _ptr(t)))
     return t
+
+
+# ---------------------------------------------------------------------------------- serving: paged cache, scoring
+
+class CacheTensors(NamedTuple):
+    """The cache of one layer: codes uint8 [num_blocks, kv_heads, block_size, d_h], scales float32 [num_blocks, kv_heads]."""
+    k_codes: torch.Tensor
+    v_codes: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+    def checked(self) -> tuple:
+        """The fields of a repq_cache, its tensors' types and layout checked."""
+        k, v, ks, vs = self
+        blocks, heads, block, d_h = k.shape
+        if v.shape != k.shape or k.dtype != torch.uint8 or v.dtype != torch.uint8 or not (k.is_contiguous() and v.is_contiguous()):
+            raise TypeError("cache codes: two dense uint8 tensors of [num_blocks, kv_heads, block_size, d_h]")
+        if ks.shape != (blocks, heads) or vs.shape != ks.shape or ks.dtype != torch.float32 or vs.dtype != torch.float32 or not (
+                ks.is_contiguous() and vs.is_contiguous()):
+            raise TypeError("cache scales: two dense float32 tensors of [num_blocks, kv_heads]")
+        return k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), blocks, heads, block, d_h
+
+
+def new_cache(num_blocks: int, kv_heads: int, block_size: int, d_h: int, device="cuda:0") -> CacheTensors:
+    """An empty cache (blocks need no clearing: what a block holds is told by the lengths of the requests)."""
+    codes = lambda: torch.empty(num_blocks, kv_heads, block_size, d_h, dtype=torch.uint8, device=device)    # noqa: E731
+    scales = lambda: torch.zeros(num_blocks, kv_heads, dtype=torch.float32, device=device)                  # noqa: E731
+    return CacheTensors(codes(), codes(), scales(), scales())
+
+
+# Descriptors of the serving entry points are packed in one go (the C layout, as the Structure classes above state it): a decode step makes
+# these calls once per layer, and filling a Structure field by field takes three times as long.
+_pack_plan = struct.Struct("@5i0P3Pq8P").pack
+_pack_write = struct.Struct("@4P4i2i0PPqqPqqP").pack
+_pack_attention = struct.Struct("@4P4i6i0PP2qPqi0P2Pf2ifi0PP2q2P").pack
+_pack_logprobs = struct.Struct("@4iPq6P").pack
+
+
+def _int32(*tensors) -> None:
+    for t in tensors:
+        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
+            raise TypeError("lengths, tables and maps are dense int32 tensors")
+
+
+def _address(t) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
+def _rows(t: torch.Tensor, what: str) -> tuple:
+    if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] != 1):
+        raise TypeError("%s: expected [tokens, heads, d_h] with consecutive elements in a head" % what)
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def repq_cache_plan(kv_lens: torch.Tensor, q_lens: torch.Tensor, block_table: torch.Tensor, free_list: torch.Tensor,
+                    free_head: torch.Tensor, block_size: int, *, kv_lens_out: torch.Tensor, cu_q: torch.Tensor,
+                    slot_map: torch.Tensor, positions: Optional[torch.Tensor], free_head_out: torch.Tensor,
+                    totals: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Block table entries, slots and positions of a step's tokens (see repq.h); every tensor int32 on the device."""
+    _int32(kv_lens, q_lens, free_list, free_head, kv_lens_out, cu_q, slot_map, positions, free_head_out, totals)
+    n, width = block_table.shape
+    if block_table.dtype != torch.int32 or (block_table.stride(1) != 1 and block_table.shape[1] > 1):
+        raise TypeError("block_table: int32 [requests, width] with dense rows")
+    if kv_lens.numel() != n or q_lens.numel() != n or kv_lens_out.numel() != n or cu_q.numel() != n + 1 or (
+            positions is not None and positions.numel() != slot_map.numel()) or (totals is not None and totals.numel() < 4):
+        raise ValueError("repq_cache_plan: sizes of the lengths, cu_q, positions or totals do not match")
+    d = _pack_plan(n, block_size, width, free_list.numel(), slot_map.numel(), kv_lens.data_ptr(), q_lens.data_ptr(),
+                   block_table.data_ptr(), block_table.stride(0), free_list.data_ptr(), free_head.data_ptr(), kv_lens_out.data_ptr(),
+                   cu_q.data_ptr(), slot_map.data_ptr(), _address(positions), free_head_out.data_ptr(), _address(totals))
+    _check(lib().repq_cache_plan(d, _stream(stream)))
+
+
+def repq_cache_write(cache: CacheTensors, k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, stream=None) -> None:
+    """K and V rows [tokens, kv_heads, d_h] (bf16 or float32, strided) quantized into the cache at slot_map's slots."""
+    _int32(slot_map)
+    c = cache.checked()
+    if k.shape != v.shape or k.dtype != v.dtype or k.shape[1:] != (c[5], c[7]) or slot_map.numel() < k.shape[0]:
+        raise ValueError("repq_cache_write: k and v are [tokens, kv_heads, d_h] of one type, slot_map has a slot per token")
+    d = _pack_write(*c, k.shape[0], _dtype_code(k), *_rows(k, "k"), *_rows(v, "v"), slot_map.data_ptr())
+    _check(lib().repq_cache_write(d, _stream(stream)))
+
+
+def _cache_attention_desc(cache, q, block_table, kv_lens, cu_q, out, max_q_len, max_kv_len, alpha, out_kind, out_bits, out_scale,
+                          out_zero, out_row_sum, lse) -> bytes:
+    c = cache.checked()
+    n, width = block_table.shape
+    o = (0, 0, 0) if out is None else _rows(out, "out")
+    return _pack_attention(*c, n, q.shape[0], q.shape[1], max_q_len, max_kv_len, _dtype_code(q), *_rows(q, "q"),
+                           block_table.data_ptr(), block_table.stride(0), width, _address(kv_lens), _address(cu_q), alpha, out_kind,
+                           out_bits, out_scale, out_zero, *o, _address(out_row_sum), _address(lse))
+
+
+def repq_cache_attention_workspace_bytes(cache: CacheTensors, q: torch.Tensor, block_table: torch.Tensor, max_q_len: int,
+                                         max_kv_len: int) -> int:
+    """Bytes of the (zero-filled) workspace of repq_cache_attention for queries of this shape and these bounds."""
+    n = C.c_size_t()
+    d = _cache_attention_desc(cache, q, block_table, None, None, None, max_q_len, max_kv_len, 1.0, 0, 8, 1.0, 0, None, None)
+    _check(lib().repq_cache_attention_workspace_bytes(d, C.byref(n)))
+    return int(n.value)
+
+
+def repq_cache_attention(cache: CacheTensors, q: torch.Tensor, block_table: torch.Tensor, kv_lens: torch.Tensor, cu_q: torch.Tensor,
+                         out: torch.Tensor, workspace: torch.Tensor, *, max_q_len: int, max_kv_len: int, alpha: float,
+                         out_bits: int = 8, out_scale: float = 1.0, out_zero: int = 0, out_row_sum: Optional[torch.Tensor] = None,
+                         lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Attention of q [tokens, heads, d_h] over the cache into out: float32 / bf16 of the same shape, or uint8 codes (out_bits,
+    out_scale, out_zero; packed 4-bit codes: last extent d_h / 2)."""
+    _int32(kv_lens, cu_q, out_row_sum)
+    if q.dim() != 3 or q.shape[2] != cache.k_codes.shape[3]:
+        raise ValueError("repq_cache_attention: q is [tokens, heads, d_h] with the cache's d_h")
+    if block_table.dtype != torch.int32 or (block_table.stride(1) != 1 and block_table.shape[1] > 1):
+        raise TypeError("block_table: int32 [requests, width] with dense rows")
+    kind = REPQ_OUT_CODES if out.dtype == torch.uint8 else REPQ_OUT_BF16 if out.dtype == torch.bfloat16 else REPQ_OUT_F32
+    if kind == REPQ_OUT_F32 and out.dtype != torch.float32:
+        raise TypeError("repq_cache_attention: out is float32, bfloat16 or uint8 codes, got %s" % out.dtype)
+    last = q.shape[2] // 2 if kind == REPQ_OUT_CODES and out_bits == 4 else q.shape[2]
+    n = block_table.shape[0]
+    if out.shape != (q.shape[0], q.shape[1], last) or kv_lens.numel() != n or cu_q.numel() != n + 1:
+        raise ValueError("repq_cache_attention: shapes of out, kv_lens or cu_q do not match q and block_table")
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape != q.shape[:2]):
+        raise TypeError("repq_cache_attention: lse is a dense float32 tensor of [tokens, heads]")
+    d = _cache_attention_desc(cache, q, block_table, kv_lens, cu_q, out, max_q_len, max_kv_len, alpha, kind, out_bits, out_scale,
+                              out_zero, out_row_sum, lse)
+    _check(lib().repq_cache_attention(d, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def repq_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], logprob: Optional[torch.Tensor] = None, *,
+                        entropy: Optional[torch.Tensor] = None, rank: Optional[torch.Tensor] = None,
+                        top_ids: Optional[torch.Tensor] = None, top_logprobs: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Log probabilities of tokens [rows] under logits [rows, vocab] (float32 or bf16), the rows' entropy, the tokens' rank and the
+    most probable alternatives (top_ids, top_logprobs [rows, top])."""
+    _int32(tokens, rank, top_ids)
+    rows, vocab = logits.shape
+    if logits.stride(1) != 1 and vocab != 1:
+        raise TypeError("repq_token_logprobs: logits are rows of consecutive elements")
+    top = 0 if top_ids is None else top_ids.shape[1]
+    for t, n in ((tokens, rows), (logprob, rows), (entropy, rows), (rank, rows), (top_ids, rows * top), (top_logprobs, rows * top)):
+        if t is not None and t.numel() != n:
+            raise ValueError("repq_token_logprobs: outputs and tokens have an entry per row (top ones `top` per row)")
+    for t in (logprob, entropy, top_logprobs):
+        if t is not None and (t.dtype != torch.float32 or not t.is_contiguous()):
+            raise TypeError("repq_token_logprobs: logprob, entropy and top_logprobs are dense float32 tensors")
+    d = _pack_logprobs(rows, vocab, top, _dtype_code(logits), logits.data_ptr(), logits.stride(0), _address(tokens), _address(logprob),
+                       _address(entropy), _address(rank), _address(top_ids), _address(top_logprobs))
+    _check(lib().repq_token_logprobs(d, _stream(stream)))
 
 
 # ---------------------------------------------------------------------------------- descriptor helpers

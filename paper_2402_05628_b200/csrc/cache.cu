@@ -1,0 +1,363 @@
+// The paged 8-bit cache: the plan of a step (block tables, slot map, positions) and the write of K / V rows.
+#include <cuda_bf16.h>
+
+#include "cache.cuh"
+#include "kernels.h"
+
+namespace repq {
+namespace cache {
+
+repq_status check(const repq_cache& c, const char* who) {
+  REPQ_REQUIRE(c.num_blocks > 0 && c.kv_heads > 0, REPQ_INVALID_ARG, "%s: num_blocks and kv_heads must be positive", who);
+  REPQ_REQUIRE(c.k_codes && c.v_codes && c.k_scale && c.v_scale, REPQ_INVALID_ARG, "%s: NULL cache pointer", who);
+  REPQ_REQUIRE(c.block_size == 16 || c.block_size == 32 || c.block_size == 64 || c.block_size == 128, REPQ_UNSUPPORTED,
+               "%s: block_size %d is not 16, 32, 64 or 128", who, c.block_size);
+  REPQ_REQUIRE(c.d_h >= 16 && c.d_h <= 128 && c.d_h % 16 == 0, REPQ_UNSUPPORTED, "%s: d_h %d is not a multiple of 16 up to 128", who, c.d_h);
+  REPQ_REQUIRE(int64_t(c.num_blocks) * c.block_size <= INT32_MAX, REPQ_UNSUPPORTED, "%s: slots of the cache pass 32 bits", who);
+  REPQ_REQUIRE(int64_t(c.num_blocks) * c.kv_heads <= INT32_MAX, REPQ_UNSUPPORTED, "%s: scales of the cache pass 32 bits", who);
+  REPQ_REQUIRE(aligned(c.k_codes, 16) && aligned(c.v_codes, 16) && aligned(c.k_scale, 4) && aligned(c.v_scale, 4), REPQ_ALIGNMENT,
+               "%s: cache codes must be 16-byte aligned", who);
+  return REPQ_OK;
+}
+
+namespace {
+
+// ---- plan.  What it costs is the latency of a few dependent reads, so there is one kernel and nothing for its CTAs to wait on: every CTA forms the two
+// prefix sums (tokens, fresh blocks) over all requests for itself, and then writes its share of the slots, CTA 0 and its neighbours also the table entries of
+// their share of the requests.
+constexpr int kPlanThreads = 512;
+constexpr int kPlanSlots = 2048;                 // slots of a CTA
+
+__device__ __forceinline__ int ceil_div_pow2(int n, int shift) { return (n >> shift) + ((n & ((1 << shift) - 1)) != 0); }
+
+struct PlanOne { int kv, q, old_blocks, fresh, lost; };
+__device__ __forceinline__ PlanOne plan_one(const repq_cache_plan_desc& d, int b, int shift) {
+  PlanOne o;
+  o.kv = max(__ldg(d.kv_lens + b), 0);
+  o.q = max(__ldg(d.q_lens + b), 0);
+  o.old_blocks = ceil_div_pow2(o.kv, shift);
+  const int all = ceil_div_pow2(o.kv + o.q, shift), in = min(all, d.table_width);
+  o.fresh = max(in - o.old_blocks, 0);
+  o.lost = max(all - max(in, o.old_blocks), 0);
+  return o;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const __grid_constant__ repq_cache_plan_desc d, int shift) {
+  __shared__ int first_token[kPlanThreads + 1], first_block[kPlanThreads];
+  __shared__ int warp_sums[4][kPlanThreads / 32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  grid_dependency_wait();
+  grid_dependency_trigger();
+  const int per = (d.requests + kPlanThreads - 1) / kPlanThreads;        // consecutive requests of a thread
+  const int b0 = min(tid * per, d.requests), b1 = min(b0 + per, d.requests);
+  int tokens = 0, blocks = 0, lost = 0, longest = 0;
+  for (int b = b0; b < b1; ++b) {
+    const PlanOne o = plan_one(d, b, shift);
+    tokens += o.q;
+    blocks += o.fresh;
+    lost += o.lost;
+    longest = max(longest, o.kv + o.q);
+  }
+  int st = tokens, sb = blocks;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int a = __shfl_up_sync(0xffffffffu, st, o), c = __shfl_up_sync(0xffffffffu, sb, o);
+    if (lane >= o) { st += a; sb += c; }
+  }
+  lost = __reduce_add_sync(0xffffffffu, lost);
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  if (lane == 31) { warp_sums[0][warp] = st; warp_sums[1][warp] = sb; warp_sums[2][warp] = lost; warp_sums[3][warp] = longest; }
+  __syncthreads();
+  int before_t = 0, before_b = 0, total_t = 0, total_b = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 32; ++w) {
+    const int a = warp_sums[0][w], c = warp_sums[1][w];
+    if (w < warp) { before_t += a; before_b += c; }
+    total_t += a;
+    total_b += c;
+  }
+  st += before_t - tokens;                       // sums before this thread's requests
+  sb += before_b - blocks;
+  first_token[tid] = st;
+  first_block[tid] = sb;
+  const int head = min(max(__ldg(d.free_head), 0), d.free_blocks);
+  const int room = d.free_blocks - head;         // entries that are left
+  if (blockIdx.x == 0) {
+    int t = st;
+    for (int b = b0; b < b1; ++b) {
+      const PlanOne o = plan_one(d, b, shift);
+      d.cu_q[b] = t;
+      d.kv_lens_out[b] = o.kv + o.q;
+      t += o.q;
+    }
+    if (tid == 0) {
+      d.cu_q[d.requests] = total_t;
+      d.free_head_out[0] = head + min(total_b, room);
+      if (d.totals) {
+        int missing = 0, most = 0;
+        for (int w = 0; w < kPlanThreads / 32; ++w) { missing += warp_sums[2][w]; most = max(most, warp_sums[3][w]); }
+        d.totals[0] = total_t;
+        d.totals[1] = min(total_b, room);
+        d.totals[2] = missing + max(total_b - room, 0);
+        d.totals[3] = most;
+      }
+    }
+  }
+  // fresh table entries: the groups of consecutive requests of the threads, dealt to the CTAs; a thread writes those of its own group
+  if (tid % gridDim.x == blockIdx.x) {
+    int e = sb;
+    for (int b = b0; b < b1; ++b) {
+      const PlanOne o = plan_one(d, b, shift);
+      int32_t* row = d.block_table + b * d.ld_table + o.old_blocks;
+      for (int i = 0; i < o.fresh; ++i, ++e) row[i] = e < room ? __ldg(d.free_list + head + e) : -1;
+    }
+  }
+  __syncthreads();
+  const int s0 = blockIdx.x * kPlanSlots;
+  for (int s = s0 + tid; s < min(s0 + kPlanSlots, d.slots); s += kPlanThreads) {
+    int slot = -1, pos = -1;
+    if (s < total_t) {
+      int lo = 0, hi = kPlanThreads - 1;         // the last group that starts at or before s
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (first_token[mid] <= s) lo = mid; else hi = mid - 1;
+      }
+      int t = first_token[lo], e = first_block[lo], b = lo * per;
+      PlanOne o = plan_one(d, b, shift);
+      while (s >= t + o.q) {
+        t += o.q;
+        e += o.fresh;
+        o = plan_one(d, ++b, shift);
+      }
+      pos = o.kv + s - t;
+      const int j = pos >> shift;
+      int page = -1;
+      if (j < d.table_width) {
+        if (j < o.old_blocks) page = d.block_table[b * d.ld_table + j];
+        else if (e + j - o.old_blocks < room) page = __ldg(d.free_list + head + e + j - o.old_blocks);
+      }
+      if (page >= 0) slot = (page << shift) + (pos & ((1 << shift) - 1));
+    }
+    d.slot_map[s] = slot;
+    if (d.positions) d.positions[s] = pos;
+  }
+}
+
+// ---- write.  Bytes are all there is to it (a row read, a row of codes written), but a block's scale needs all of the rows that it gets: a warp takes one
+// head's K or V rows of one block ("run"), 16 of them at a time in registers where they fit.  CTAs take windows of consecutive tokens, so that the
+// tokens that do not start a run cost a vote and no launch.
+constexpr int kWriteWarps = 8;
+
+struct WriteParams {
+  repq_cache c;
+  const void* x[2];
+  int64_t st[2], sh[2];
+  const int32_t* slots;
+  int tokens, shift, window, tasks;               // tasks: kv_heads * 2
+};
+
+__device__ __forceinline__ float magnitude(float a) { return fminf(fabsf(a), 3.402823466e38f); }   // (fminf drops a NaN ...)
+
+// round(x / s) to a code, as the IEEE quotient rounds: x * (1 / s) is within 2^-15 of it where codes are, so only quotients near a tie are divided
+__device__ __forceinline__ uint32_t code_of(float x, float s, float inv) {
+  float t = x * inv, q = rintf(t);
+  if (fabsf(fabsf(t - q) - 0.5f) < 1e-4f) q = rintf(__fdiv_rn(x, s));
+  q = fminf(fmaxf(q, -127.f), 127.f);
+  return x == x ? uint32_t(int(q) + 128) : 128u;
+}
+
+template <typename T> struct Piece;               // eight elements
+template <> struct Piece<__nv_bfloat16> {
+  uint4 r;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { r = __ldg(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void clear() { r = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+  }
+};
+template <> struct Piece<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = __ldg(reinterpret_cast<const float4*>(p));
+    b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  }
+  __device__ __forceinline__ void clear() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  }
+};
+
+// kHeld pieces of eight elements per lane stay in registers between the maximum and the codes; a run of more rows reads them again.
+template <typename T, int kHeld>
+__global__ void __launch_bounds__(32 * kWriteWarps) cache_write_kernel(const __grid_constant__ WriteParams P) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int task = blockIdx.y * kWriteWarps + warp;
+  grid_dependency_wait();
+  grid_dependency_trigger();
+  if (task >= P.tasks) return;
+  const int head = task >> 1, kv = task & 1;
+  const int bs = 1 << P.shift, pieces = P.c.d_h >> 3;
+  const int t_end = min((int(blockIdx.x) + 1) * P.window, P.tokens);
+  const int64_t slots = int64_t(P.c.num_blocks) << P.shift;
+  const T* base = static_cast<const T*>(kv ? P.x[1] : P.x[0]) + head * (kv ? P.sh[1] : P.sh[0]);
+  const int64_t st = kv ? P.st[1] : P.st[0];
+  uint8_t* codes_base = kv ? P.c.v_codes : P.c.k_codes;
+  float* scale_base = kv ? P.c.v_scale : P.c.k_scale;
+  for (int w0 = int(blockIdx.x) * P.window; w0 < t_end; w0 += 32) {
+    const int t = w0 + lane;
+    bool starts = false;
+    if (t < t_end) {
+      const int s = __ldg(P.slots + t);
+      starts = s >= 0 && s < slots && (t == 0 || (s & (bs - 1)) == 0 || __ldg(P.slots + t - 1) != s - 1);
+    }
+    uint32_t todo = __ballot_sync(0xffffffffu, starts);
+    while (todo) {
+      const int t0 = w0 + __ffs(todo) - 1;
+      todo &= todo - 1;
+      const int slot0 = __ldg(P.slots + t0), off = slot0 & (bs - 1), page = slot0 >> P.shift;
+      int rows = 0;                                // of the run: consecutive slots up to the block's end
+      for (; rows < bs - off; rows += 32) {
+        const int i = rows + lane;
+        const bool in = i < bs - off && t0 + i < P.tokens && __ldg(P.slots + t0 + i) == slot0 + i;
+        const uint32_t m = ~__ballot_sync(0xffffffffu, in);
+        if (m) { rows += __ffs(m) - 1; break; }
+      }
+      rows = min(rows, bs - off);
+      const int64_t tile = int64_t(page) * P.c.kv_heads + head;
+      uint8_t* codes = codes_base + (tile << P.shift) * P.c.d_h;
+      const float before = off ? scale_base[tile] : 0.f;
+      const T* x = base + t0 * st;
+      const int n = rows * pieces;                 // pieces of the run
+      float top = 0.f;
+      Piece<T> held[kHeld];
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        const int e = lane + 32 * i;
+        if (e < n) { const int r = e / pieces; held[i].load(x + r * st + 8 * (e - r * pieces)); }
+        else held[i].clear();
+      }
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        held[i].get(f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = fmaxf(top, f[k] == f[k] ? magnitude(f[k]) : 0.f);
+      }
+      for (int e = lane + 32 * kHeld; e < n; e += 32) {
+        Piece<T> p;
+        const int r = e / pieces;
+        p.load(x + r * st + 8 * (e - r * pieces));
+        p.get(f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = fmaxf(top, f[k] == f[k] ? magnitude(f[k]) : 0.f);
+      }
+      // (magnitudes order as their bits do)
+      top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+      const float after = fmaxf(before, fmaxf(__fmul_rn(top, 1.0f / 127.0f), 0x1p-60f));
+      if (after > before) {
+        if (off) {                                 // the block's earlier rows move to the wider scale
+          const float ratio = __fdiv_rn(before, after);
+          uint32_t* w = reinterpret_cast<uint32_t*>(codes);
+          for (int e = lane; e < (off * P.c.d_h) >> 2; e += 32) {
+            const uint32_t u = w[e];
+            uint32_t o = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float c = fminf(fmaxf(rintf(__fmul_rn(float(int((u >> (8 * k)) & 255u) - 128), ratio)), -127.f), 127.f);
+              o |= uint32_t(int(c) + 128) << (8 * k);
+            }
+            w[e] = o;
+          }
+        }
+        if (lane == 0) scale_base[tile] = after;
+      }
+      const float inv = __fdiv_rn(1.0f, after);
+      uint2* to = reinterpret_cast<uint2*>(codes + off * P.c.d_h);
+      auto put = [&](const Piece<T>& p, int e) {
+        p.get(f);
+        uint32_t c[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) c[k] = code_of(f[k], after, inv);
+        uint2 o;
+        o.x = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+        o.y = __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410);
+        to[e] = o;                                 // (rows of codes are dense: piece e of the run is 8 e bytes in)
+      };
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i)
+        if (lane + 32 * i < n) put(held[i], lane + 32 * i);
+      for (int e = lane + 32 * kHeld; e < n; e += 32) {
+        Piece<T> p;
+        const int r = e / pieces;
+        p.load(x + r * st + 8 * (e - r * pieces));
+        put(p, e);
+      }
+    }
+  }
+}
+
+template <typename T>
+repq_status launch_write(const WriteParams& P, cudaStream_t st) {
+  const dim3 grid((P.tokens + P.window - 1) / P.window, (P.tasks + kWriteWarps - 1) / kWriteWarps);
+  if (P.window == 1) REPQ_CUDA(launch_chained(cache_write_kernel<T, 1>, grid, dim3(32 * kWriteWarps), 0, st, P));
+  else REPQ_CUDA(launch_chained(cache_write_kernel<T, 8>, grid, dim3(32 * kWriteWarps), 0, st, P));
+  note_launch();
+  return REPQ_OK;
+}
+
+}  // namespace
+}  // namespace cache
+}  // namespace repq
+
+using namespace repq;
+
+extern "C" repq_status repq_cache_plan(const repq_cache_plan_desc* d, void* stream) {
+  REPQ_REQUIRE(d != nullptr, REPQ_INVALID_ARG, "repq_cache_plan: NULL descriptor");
+  REPQ_REQUIRE(d->requests >= 0 && d->table_width >= 0 && d->free_blocks >= 0 && d->slots >= 0, REPQ_INVALID_ARG,
+               "repq_cache_plan: negative size");
+  const int bs = d->block_size;
+  REPQ_REQUIRE(bs == 16 || bs == 32 || bs == 64 || bs == 128, REPQ_UNSUPPORTED, "repq_cache_plan: block_size %d is not 16, 32, 64 or 128", bs);
+  REPQ_REQUIRE(d->cu_q && d->free_head && d->free_head_out, REPQ_INVALID_ARG, "repq_cache_plan: NULL pointer");
+  REPQ_REQUIRE(d->requests == 0 || (d->kv_lens && d->q_lens && d->kv_lens_out), REPQ_INVALID_ARG, "repq_cache_plan: NULL lengths");
+  REPQ_REQUIRE(d->requests == 0 || (d->kv_lens_out != d->kv_lens && d->kv_lens_out != d->q_lens), REPQ_INVALID_ARG,
+               "repq_cache_plan: kv_lens_out must not be an input (every CTA reads all lengths)");
+  REPQ_REQUIRE(d->free_head_out != d->free_head, REPQ_INVALID_ARG, "repq_cache_plan: free_head_out must not be free_head");
+  REPQ_REQUIRE(d->table_width == 0 || d->requests == 0 || d->block_table, REPQ_INVALID_ARG, "repq_cache_plan: NULL block_table");
+  REPQ_REQUIRE(d->free_blocks == 0 || d->free_list, REPQ_INVALID_ARG, "repq_cache_plan: NULL free_list");
+  REPQ_REQUIRE(d->slots == 0 || d->slot_map, REPQ_INVALID_ARG, "repq_cache_plan: NULL slot_map");
+  REPQ_REQUIRE(d->ld_table >= d->table_width, REPQ_INVALID_ARG, "repq_cache_plan: ld_table is smaller than table_width");
+  const int shift = bs == 16 ? 4 : bs == 32 ? 5 : bs == 64 ? 6 : 7;
+  const int grid = d->slots > cache::kPlanSlots ? (d->slots + cache::kPlanSlots - 1) / cache::kPlanSlots : 1;
+  REPQ_CUDA(launch_chained(cache::cache_plan_kernel, dim3(grid), dim3(cache::kPlanThreads), 0, static_cast<cudaStream_t>(stream), *d, shift));
+  note_launch();
+  return REPQ_OK;
+}
+
+extern "C" repq_status repq_cache_write(const repq_cache_write_desc* d, void* stream) {
+  REPQ_REQUIRE(d != nullptr, REPQ_INVALID_ARG, "repq_cache_write: NULL descriptor");
+  REPQ_TRY(cache::check(d->cache, "repq_cache_write"));
+  REPQ_REQUIRE(d->tokens >= 0, REPQ_INVALID_ARG, "repq_cache_write: negative number of tokens");
+  REPQ_REQUIRE(d->dtype == REPQ_F32 || d->dtype == REPQ_BF16, REPQ_INVALID_ARG, "repq_cache_write: dtype %d", d->dtype);
+  if (d->tokens == 0) return REPQ_OK;
+  REPQ_REQUIRE(d->k && d->v && d->slot_map, REPQ_INVALID_ARG, "repq_cache_write: NULL pointer");
+  const int64_t unit = d->dtype == REPQ_F32 ? 4 : 2;
+  REPQ_REQUIRE(aligned(d->k, 16) && aligned(d->v, 16) && (d->k_stride_token | d->k_stride_head | d->v_stride_token | d->v_stride_head) * unit % 16 == 0,
+               REPQ_ALIGNMENT, "repq_cache_write: rows of k and v must be 16-byte aligned");
+  cache::WriteParams P;
+  P.c = d->cache;
+  P.x[0] = d->k; P.st[0] = d->k_stride_token; P.sh[0] = d->k_stride_head;
+  P.x[1] = d->v; P.st[1] = d->v_stride_token; P.sh[1] = d->v_stride_head;
+  P.slots = d->slot_map;
+  P.tokens = d->tokens;
+  P.shift = cache::log2_block(d->cache.block_size);
+  P.tasks = 2 * d->cache.kv_heads;
+  // a window per CTA such that there are some 32 warps per SM; one token where there are few
+  const int64_t per = int64_t(d->tokens) * P.tasks / (int64_t(sm_count()) * 32);
+  P.window = 1;
+  while (P.window < per && P.window < 128) P.window *= 2;
+  REPQ_REQUIRE((P.tasks + 7) / 8 <= 65535, REPQ_UNSUPPORTED, "repq_cache_write: too many heads");
+  return d->dtype == REPQ_F32 ? cache::launch_write<float>(P, static_cast<cudaStream_t>(stream))
+                              : cache::launch_write<__nv_bfloat16>(P, static_cast<cudaStream_t>(stream));
+}

@@ -1,0 +1,90 @@
+// repq_cache_attention: checks and dispatch.
+#include "cache_attention.cuh"
+
+namespace repq {
+namespace cache {
+namespace {
+
+repq_status prepare(const repq_cache_attention_desc* d, AttendParams* out, bool* precise) {
+  REPQ_REQUIRE(d != nullptr, REPQ_INVALID_ARG, "repq_cache_attention: NULL descriptor");
+  REPQ_TRY(check(d->cache, "repq_cache_attention"));
+  REPQ_REQUIRE(d->requests >= 0 && d->tokens >= 0 && d->heads > 0, REPQ_INVALID_ARG, "repq_cache_attention: sizes");
+  REPQ_REQUIRE(d->heads % d->cache.kv_heads == 0, REPQ_INVALID_ARG, "repq_cache_attention: %d heads do not divide into %d key / value heads",
+               d->heads, d->cache.kv_heads);
+  REPQ_REQUIRE(d->max_q_len >= 0 && d->max_kv_len >= 0, REPQ_INVALID_ARG, "repq_cache_attention: negative bounds");
+  REPQ_REQUIRE(int64_t(d->max_q_len) * (d->heads / d->cache.kv_heads) <= (1 << 30), REPQ_UNSUPPORTED, "repq_cache_attention: max_q_len %d", d->max_q_len);
+  REPQ_REQUIRE(d->q_dtype == REPQ_F32 || d->q_dtype == REPQ_BF16, REPQ_INVALID_ARG, "repq_cache_attention: q_dtype %d", d->q_dtype);
+  REPQ_REQUIRE(d->table_width >= 0 && (d->ld_table >= d->table_width || d->requests <= 1), REPQ_INVALID_ARG,
+               "repq_cache_attention: ld_table is smaller than table_width");
+  AttendParams P = {};
+  P.c = d->cache;
+  P.shift = log2_block(d->cache.block_size);
+  P.requests = d->requests; P.tokens = d->tokens; P.heads = d->heads; P.group = d->heads / d->cache.kv_heads;
+  // no request holds more tokens than its table row has entries for
+  const int64_t room = int64_t(d->table_width) << P.shift;
+  P.max_q = d->max_q_len < d->tokens ? d->max_q_len : d->tokens;
+  P.max_kv = d->max_kv_len < room ? d->max_kv_len : int(room);
+  P.q = d->q; P.q_st = d->q_stride_token; P.q_sh = d->q_stride_head;
+  P.table = d->block_table; P.ld_table = d->ld_table; P.table_width = d->table_width;
+  P.kv_lens = d->kv_lens; P.cu_q = d->cu_q;
+  P.scale = d->alpha * 1.4426950408889634f;
+  P.out_kind = d->out_kind;
+  P.out = d->out; P.ldo = d->ldo; P.o_sh = d->o_stride_head;
+  P.out_row_sum = nullptr;
+  P.lse = d->lse;
+  if (d->out_kind == REPQ_OUT_CODES) {
+    REPQ_REQUIRE(bits_ok(d->out_bits), REPQ_INVALID_ARG, "repq_cache_attention: out_bits %d", d->out_bits);
+    REPQ_REQUIRE(d->out_scale > 0.f, REPQ_INVALID_ARG, "repq_cache_attention: out_scale must be positive");
+    P.qmax = code_max(d->out_bits);
+    P.pack4 = packed4(d->out_bits);
+    P.inv_so = 1.0f / d->out_scale;
+    P.zo = d->out_zero;
+    P.out_row_sum = d->out_row_sum;
+  } else {
+    REPQ_REQUIRE(d->out_kind == REPQ_OUT_F32 || d->out_kind == REPQ_OUT_BF16, REPQ_INVALID_ARG, "repq_cache_attention: out_kind %d", d->out_kind);
+  }
+  *precise = d->q_dtype == REPQ_F32;
+  *out = P;
+  return REPQ_OK;
+}
+
+bool nothing(const AttendParams& P) { return P.requests == 0 || P.max_q == 0; }
+
+}  // namespace
+}  // namespace cache
+}  // namespace repq
+
+using namespace repq;
+
+extern "C" repq_status repq_cache_attention_workspace_bytes(const repq_cache_attention_desc* d, size_t* bytes) {
+  REPQ_REQUIRE(bytes != nullptr, REPQ_INVALID_ARG, "repq_cache_attention_workspace_bytes: NULL pointer");
+  *bytes = 0;
+  cache::AttendParams P;
+  bool precise;
+  REPQ_TRY(cache::prepare(d, &P, &precise));
+  if (cache::nothing(P)) return REPQ_OK;
+  cache::RowsPlan plan;
+  REPQ_TRY(cache::rows_plan(P, precise, &plan));
+  *bytes = plan.workspace;
+  return REPQ_OK;
+}
+
+extern "C" repq_status repq_cache_attention(const repq_cache_attention_desc* d, void* workspace, size_t workspace_bytes, void* stream) {
+  cache::AttendParams P;
+  bool precise;
+  REPQ_TRY(cache::prepare(d, &P, &precise));
+  if (cache::nothing(P)) return REPQ_OK;
+  REPQ_REQUIRE(d->q && d->out && d->kv_lens && d->cu_q && (d->block_table || P.max_kv == 0), REPQ_INVALID_ARG, "repq_cache_attention: NULL pointer");
+  const int64_t unit = d->q_dtype == REPQ_F32 ? 4 : 2;
+  REPQ_REQUIRE(aligned(d->q, 16) && (d->q_stride_token | d->q_stride_head) * unit % 16 == 0, REPQ_ALIGNMENT,
+               "repq_cache_attention: rows of q must be 16-byte aligned");
+  const int64_t out_unit = d->out_kind == REPQ_OUT_F32 ? 4 : d->out_kind == REPQ_OUT_BF16 ? 2 : 1, out_align = d->out_kind == REPQ_OUT_CODES ? 4 : 16;
+  REPQ_REQUIRE(aligned(d->out, out_align) && (d->ldo | d->o_stride_head) * out_unit % out_align == 0, REPQ_ALIGNMENT,
+               "repq_cache_attention: rows of out must be %d-byte aligned", int(out_align));
+  cache::RowsPlan plan;
+  REPQ_TRY(cache::rows_plan(P, precise, &plan));
+  REPQ_REQUIRE(plan.workspace == 0 || (workspace && workspace_bytes >= plan.workspace), REPQ_WORKSPACE_TOO_SMALL,
+               "repq_cache_attention: workspace of %zu bytes, %zu are needed", workspace_bytes, plan.workspace);
+  REPQ_REQUIRE(aligned(workspace, 16), REPQ_ALIGNMENT, "repq_cache_attention: workspace must be 16-byte aligned");
+  return cache::launch_rows(P, precise, workspace, static_cast<cudaStream_t>(stream));
+}

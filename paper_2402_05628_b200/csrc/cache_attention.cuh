@@ -1,0 +1,90 @@
+// What the attention kernels over the 8-bit cache share: parameters, conversions, the output.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math_constants.h>
+
+#include "cache.cuh"
+#include "kernels.h"
+
+namespace repq {
+namespace cache {
+
+struct AttendParams {
+  repq_cache c;
+  int shift;                             // log2 block_size
+  int requests, tokens, heads, group;    // group: query heads of a key / value head
+  int max_q, max_kv;
+  const void* q; int64_t q_st, q_sh;
+  const int32_t* table; int64_t ld_table; int table_width;
+  const int32_t* kv_lens; const int32_t* cu_q;
+  float scale;                           // alpha log2 e
+  int out_kind, qmax, pack4;
+  float inv_so; int zo;
+  void* out; int64_t ldo, o_sh;
+  int32_t* out_row_sum;
+  float* lse;
+  int32_t* counters;                     // workspace: one per worker, zero between calls
+  float* partials;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float lg2(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ uint32_t bits_of(const __half2& h) { return *reinterpret_cast<const uint32_t*>(&h); }
+__device__ __forceinline__ __half2 half2_of(const uint32_t& w) { return *reinterpret_cast<const __half2*>(&w); }
+
+// Codes 0..255 become f16 numbers by the bytes alone: 0x6400 | c is 1024 + c, and 1024 + c - 1152 = c - 128 is exact.
+__device__ __forceinline__ uint32_t codes_lo(uint32_t w) {        // bytes 0 and 1
+  return bits_of(__hsub2(half2_of(__byte_perm(w, 0x64646464u, 0x4140)), __half2half2(__ushort_as_half(0x6480))));
+}
+__device__ __forceinline__ uint32_t codes_hi(uint32_t w) {        // bytes 2 and 3
+  return bits_of(__hsub2(half2_of(__byte_perm(w, 0x64646464u, 0x4342)), __half2half2(__ushort_as_half(0x6480))));
+}
+
+// What a request asks for, lengths taken within the bounds of the call.
+struct Request { int q0, q_len, q_true, kv; };
+__device__ __forceinline__ Request request_of(const AttendParams& P, int b) {
+  Request r;
+  r.q0 = min(max(__ldg(P.cu_q + b), 0), P.tokens);
+  const int q1 = min(max(__ldg(P.cu_q + b + 1), r.q0), P.tokens);
+  r.q_true = q1 - r.q0;
+  r.q_len = min(r.q_true, P.max_q);
+  r.kv = max(__ldg(P.kv_lens + b), 0);
+  return r;
+}
+
+// Two neighbouring channels of an output row; the codes' sum for the row sums.
+__device__ __forceinline__ int store_pair(const AttendParams& P, int token, int head, int d, float a, float b) {
+  const int64_t at = token * P.ldo + head * P.o_sh;
+  if (P.out_kind == REPQ_OUT_F32) {
+    *reinterpret_cast<float2*>(static_cast<float*>(P.out) + at + d) = make_float2(a, b);
+    return 0;
+  }
+  if (P.out_kind == REPQ_OUT_BF16) {
+    *reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(P.out) + at + d) = __floats2bfloat162_rn(a, b);
+    return 0;
+  }
+  const float lo = float(-P.zo), hi = float(P.qmax - P.zo);
+  const int ca = __float2int_rn(fminf(fmaxf(a * P.inv_so, lo), hi)) + P.zo, cb = __float2int_rn(fminf(fmaxf(b * P.inv_so, lo), hi)) + P.zo;
+  uint8_t* o = static_cast<uint8_t*>(P.out) + at;
+  if (P.pack4) o[d >> 1] = uint8_t(ca | cb << 4);
+  else *reinterpret_cast<uint16_t*>(o + d) = uint16_t(ca | cb << 8);
+  return ca + cb;
+}
+
+// The kernel for a few rows per key / value head (cache_attention_rows.cu): how it would be launched, and the launch.
+struct RowsPlan { int row_tiles, workers; size_t counter_bytes, workspace; };
+repq_status rows_plan(const AttendParams& P, bool precise, RowsPlan* plan);
+repq_status launch_rows(AttendParams P, bool precise, void* workspace, cudaStream_t st);
+
+}  // namespace cache
+}  // namespace repq

@@ -1,0 +1,485 @@
+// Attention over the 8-bit cache for a few rows per key / value head: decode steps, tokens to verify, short chunks, float32 queries.
+//
+// Rows are the queries of one request that read one key / value head (token x group); a job is up to 8 kTiles of them against
+// the keys they see, in units of 64 keys, 16 per warp.  All jobs' units form one line, cut into equal shares for as many CTAs as the
+// GPU holds: a share may begin and end inside a job, so that few rows over a long axis and many requests of different lengths fill
+// the SMs alike.  A job that lies in several shares is joined by whichever CTA finishes last (a counter per job; parts are read in
+// order, so results do not depend on which CTA that is).
+//
+// A warp multiplies on mma.m16n8k16 in f16 with float32 sums, keys and channels on the M side, rows on the N side:
+//     S^T [16 keys x 8 rows] = K [16 x d_h] Q^T,      O^T [d_h x 8 rows] += V^T [d_h x 16 keys] P^T.
+// Codes minus 128 are f16 numbers exactly.  The contraction's order is free, so a thread loads its operands straight from the
+// cache in 16-byte pieces (K: d_h / 4 consecutive bytes of two keys; V: d_h / 8 consecutive channels of four keys, transposed
+// by byte permutations that the conversion needs anyway); nothing passes through shared memory until the end of a job.
+//
+// With x = S alpha k_scale log2 e, a row keeps m, the largest x + log2 v_scale seen, Z = sum 2^(x - m + 15) and
+// O = sum 2^(x - m + 15) v_scale (c - 128): weights of the second product lie in f16's range whatever the blocks' scales are, with
+// 11 bits down to 2^-29 of the largest (float32 queries: queries and weights as two f16 numbers each, 22 bits).
+#pragma once
+#include "cache_attention.cuh"
+
+namespace repq {
+namespace cache {
+namespace rows {
+
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kUnit = 16 * kWarps;                // keys of a unit
+constexpr float kLift = 15.f;                     // exponent of the largest weight: f16's normal range then holds weights down to 2^-29 of it
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_half(float a, float b) { return bits_of(__floats2half2_rn(a, b)); }
+__device__ __forceinline__ float2 unpack_half(uint32_t w) { return __half22float2(half2_of(w)); }
+
+// kWords consecutive words, by the widest loads their alignment (the step between threads) allows; the cache is read once
+template <int kWords> __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[kWords]) {
+  if constexpr (kWords % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < kWords / 4; ++i)
+      asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3]) : "l"(p + 16 * i));
+  } else if constexpr (kWords % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < kWords / 2; ++i)
+      asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[2 * i]), "=r"(w[2 * i + 1]) : "l"(p + 8 * i));
+  } else {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(w[i]) : "l"(p + 4 * i));
+  }
+}
+
+template <int kSteps>                             // d_h / 16
+struct Keys {
+  static constexpr int kV = (kSteps + 1) / 2;
+  uint32_t k[2][kSteps], v[4][kV];
+  float ks, vs;
+  bool there;
+  __device__ __forceinline__ void load(const AttendParams& P, int page, int h, int off, int g, int t) {
+    there = unsigned(page) < unsigned(P.c.num_blocks);
+    if (!there) return;
+    constexpr int dh = 16 * kSteps;
+    const int64_t tile = int64_t(page) * P.c.kv_heads + h;
+    const uint8_t* kp = P.c.k_codes + ((tile << P.shift) + off) * dh + g * dh + t * (4 * kSteps);
+    load_words<kSteps>(kp, k[0]);
+    load_words<kSteps>(kp + 8 * dh, k[1]);
+    const uint8_t* vp = P.c.v_codes + ((tile << P.shift) + off) * dh + 2 * t * dh + g * (2 * kSteps);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint8_t* p = vp + ((i & 1) + 8 * (i >> 1)) * dh;
+      if constexpr (kSteps % 2 == 0) load_words<kV>(p, v[i]);
+      else {
+#pragma unroll
+        for (int j = 0; j < kV; ++j)
+          v[i][j] = uint32_t(__ldg(reinterpret_cast<const uint16_t*>(p) + 2 * j)) |
+                    (2 * j + 1 < kSteps ? uint32_t(__ldg(reinterpret_cast<const uint16_t*>(p) + 2 * j + 1)) << 16 : 0u);
+      }
+    }
+    ks = __ldg(P.c.k_scale + tile);
+    vs = __ldg(P.c.v_scale + tile);
+  }
+};
+
+// A warp's rows: queries as B fragments, running statistics of its columns, accumulators.
+template <int kSteps, int kTiles, bool kPrecise>
+struct Rows {
+  uint32_t q[kTiles][2 * kSteps], ql[kPrecise ? kTiles : 1][kPrecise ? 2 * kSteps : 1];
+  float back[kTiles][2];                          // of the two columns: what undoes the queries' scaling, times alpha log2 e
+  float m[kTiles][2], z[kTiles][2];
+  float o[kTiles][kSteps][4];
+  int limit[kTiles][2];                           // keys that the column's row sees
+
+  template <typename T>
+  __device__ __forceinline__ void load_row(const AttendParams& P, const Request& rq, int h, int row, int n_rows, int t, int i, float& factor) {
+    float f[4 * kSteps];
+    const int token = row / P.group;
+    const T* p = static_cast<const T*>(P.q) + (rq.q0 + token) * P.q_st + (h * P.group + row - token * P.group) * P.q_sh + t * (4 * kSteps);
+    const bool in = row < n_rows;
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+      if constexpr (sizeof(T) == 4) {
+        const float4 w = in ? __ldg(reinterpret_cast<const float4*>(p) + j) : make_float4(0.f, 0.f, 0.f, 0.f);
+        f[4 * j] = w.x; f[4 * j + 1] = w.y; f[4 * j + 2] = w.z; f[4 * j + 3] = w.w;
+      } else {
+        const uint2 w = in ? __ldg(reinterpret_cast<const uint2*>(p) + j) : make_uint2(0u, 0u);
+        f[4 * j] = __uint_as_float(w.x << 16); f[4 * j + 1] = __uint_as_float(w.x & 0xffff0000u);
+        f[4 * j + 2] = __uint_as_float(w.y << 16); f[4 * j + 3] = __uint_as_float(w.y & 0xffff0000u);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(f[4 * j + e]));
+    }
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    // the row's largest element comes to lie in [2^8, 2^9): f16 then holds bf16 elements exactly down to 2^-22 of it
+    const int e = min(max(int(__float_as_uint(top) >> 23) - 127 - 8, -110), 110);
+    const float down = __uint_as_float(uint32_t(127 - e) << 23);
+    factor = __uint_as_float(uint32_t(127 + e) << 23) * P.scale;
+#pragma unroll
+    for (int j = 0; j < 2 * kSteps; ++j) {
+      const float a = f[2 * j] * down, b = f[2 * j + 1] * down;
+      q[i][j] = pack_half(a, b);
+      if constexpr (kPrecise) {
+        const float2 hi = unpack_half(q[i][j]);
+        ql[i][j] = pack_half(a - hi.x, b - hi.y);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void begin(const AttendParams& P, const Request& rq, int h, int row0, int n_rows, int g, int t) {
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+      float factor;
+      const int row = row0 + 8 * i + g;
+      if constexpr (kPrecise) load_row<float>(P, rq, h, row, n_rows, t, i, factor);
+      else load_row<__nv_bfloat16>(P, rq, h, row, n_rows, t, i, factor);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        back[i][c] = __shfl_sync(0xffffffffu, factor, 4 * (2 * t + c));     // (lane of row 2 t + c)
+        const int col = row0 + 8 * i + 2 * t + c;
+        limit[i][c] = col < n_rows ? min(rq.kv - rq.q_true + col / P.group + 1, P.max_kv) : 0;
+        m[i][c] = -CUDART_INF_F;
+        z[i][c] = 0.f;
+      }
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][s][e] = 0.f;
+    }
+  }
+
+  // 16 keys from k0 on
+  __device__ __forceinline__ void take(const Keys<kSteps>& K, int k0, int g) {
+    if (!K.there) return;
+    float s[kTiles][4];
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[i][e] = 0.f;
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+      const uint32_t a[4] = {codes_lo(K.k[0][j]), codes_lo(K.k[1][j]), codes_hi(K.k[0][j]), codes_hi(K.k[1][j])};
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) {
+        mma(s[i], a, q[i][2 * j], q[i][2 * j + 1]);
+        if constexpr (kPrecise) mma(s[i], a, ql[i][2 * j], ql[i][2 * j + 1]);
+      }
+    }
+    const float lvs = lg2(K.vs);
+    bool rises = false;
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const float f = K.ks * back[i][c];
+        s[i][c] = k0 + g < limit[i][c] ? s[i][c] * f : -CUDART_INF_F;
+        s[i][2 + c] = k0 + 8 + g < limit[i][c] ? s[i][2 + c] * f : -CUDART_INF_F;
+        rises = rises || fmaxf(s[i][c], s[i][2 + c]) + lvs > m[i][c];
+      }
+    if (__any_sync(0xffffffffu, rises)) {
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float top = fmaxf(s[i][c], s[i][2 + c]) + lvs;
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+          if (top > m[i][c]) {
+            const float f = ex2(m[i][c] - top);
+            m[i][c] = top;
+            z[i][c] *= f;
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j) { o[i][j][c] *= f; o[i][j][2 + c] *= f; }
+          }
+        }
+    }
+    uint32_t p[kTiles][2], pl[kPrecise ? kTiles : 1][2];
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+      float w[4];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const float base = m[i][c] == -CUDART_INF_F ? 0.f : kLift - m[i][c];
+        const float a = ex2(s[i][c] + base), b = ex2(s[i][2 + c] + base);
+        z[i][c] += a + b;
+        w[c] = a * K.vs;
+        w[2 + c] = b * K.vs;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t hi = pack_half(w[2 * e], w[2 * e + 1]);
+        p[i][e] = transposed(hi);
+        if constexpr (kPrecise) {
+          const float2 f = unpack_half(hi);
+          pl[i][e] = transposed(pack_half(w[2 * e] - f.x, w[2 * e + 1] - f.y));
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kSteps; j += 2) {
+      // bytes of the key pairs (2t, 2t + 1) and (2t + 8, 2t + 9) brought together: channels 0 1 of the word, then 2 3
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if (j + u < kSteps) {
+          const uint32_t sel = u ? 0x7362u : 0x5140u;
+          const uint32_t x = __byte_perm(K.v[0][j / 2], K.v[1][j / 2], sel), y = __byte_perm(K.v[2][j / 2], K.v[3][j / 2], sel);
+          const uint32_t a[4] = {codes_lo(x), codes_hi(x), codes_lo(y), codes_hi(y)};
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i) {
+            mma(o[i][j + u], a, p[i][0], p[i][1]);
+            if constexpr (kPrecise) mma(o[i][j + u], a, pl[i][0], pl[i][1]);
+          }
+        }
+      }
+    }
+  }
+};
+
+template <int kSteps, int kTiles>
+struct Shared {
+  static constexpr int kRows = 8 * kTiles, kRow = 16 * kSteps + 8;      // (padded against bank conflicts)
+  float o[kWarps][kRows][kRow];
+  float m[kWarps][kRows], z[kWarps][kRows];
+  int sums[kRows];
+  long long first[kThreads + 1];                  // units before a thread's requests
+  int last;
+};
+
+// units of 64 keys that the tiles of one key / value head of a request take
+struct Share { int tiles, units; };
+__device__ __forceinline__ Share share_of(const AttendParams& P, const Request& rq, int tile_rows) {
+  Share s;
+  s.tiles = (rq.q_len * P.group + tile_rows - 1) / tile_rows;
+  s.units = max((min(rq.kv, P.max_kv) + kUnit - 1) / kUnit, 1);
+  return s;
+}
+
+template <int kSteps, int kTiles, bool kPrecise>
+__global__ void __launch_bounds__(kThreads, kTiles == 1 && !kPrecise ? 4 : 3) cache_rows_kernel(const __grid_constant__ AttendParams P) {
+  constexpr int kRowsOf = 8 * kTiles, dh = 16 * kSteps, kPart = kRowsOf * (dh + 2);
+  __shared__ Shared<kSteps, kTiles> S;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  grid_dependency_wait();
+  grid_dependency_trigger();
+
+  // ---- the line of units: requests in order, of one the key / value heads, of one the row tiles
+  const int per = (P.requests + kThreads - 1) / kThreads;
+  {
+    long long n = 0;
+    for (int b = tid * per; b < min((tid + 1) * per, P.requests); ++b) {
+      const Share s = share_of(P, request_of(P, b), kRowsOf);
+      n += (long long)s.tiles * s.units * P.c.kv_heads;
+    }
+    long long before = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long a = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += a;
+    }
+    if (lane == 31) S.first[warp] = before;       // (warps' sums for a moment)
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) before += S.first[w];
+    __syncthreads();
+    S.first[tid + 1] = before;
+    if (tid == 0) S.first[0] = 0;
+    __syncthreads();
+  }
+  const long long total = S.first[kThreads];
+  const long long workers = min((long long)gridDim.x, total);
+  if (blockIdx.x >= workers) return;
+  long long at = blockIdx.x * total / workers;
+  const long long end = (blockIdx.x + 1) * total / workers;
+
+  int b;
+  long long start;                                // of request b on the line
+  {
+    int lo = 0, hi = kThreads - 1;                // the last group of requests that starts at or before `at`
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (S.first[mid] <= at) lo = mid; else hi = mid - 1;
+    }
+    b = lo * per;
+    start = S.first[lo];
+  }
+  Request rq = request_of(P, b);
+  Share sh = share_of(P, rq, kRowsOf);
+  while (at < end) {
+    while (at >= start + (long long)sh.tiles * sh.units * P.c.kv_heads) {
+      start += (long long)sh.tiles * sh.units * P.c.kv_heads;
+      rq = request_of(P, ++b);
+      sh = share_of(P, rq, kRowsOf);
+    }
+    const int job = int((at - start) / sh.units), u0 = int(at - start - (long long)job * sh.units);
+    const int u1 = int(min((long long)sh.units, u0 + (end - at)));
+    const int h = job / sh.tiles, row0 = (job - h * sh.tiles) * kRowsOf, n_rows = rq.q_len * P.group, live = min(n_rows - row0, kRowsOf);
+
+    Rows<kSteps, kTiles, kPrecise> R;
+    R.begin(P, rq, h, row0, n_rows, g, t);
+    // keys that the tile's last row sees, within the table
+    const int seen = min(min(rq.kv - rq.q_true + (row0 + live - 1) / P.group + 1, rq.kv), P.max_kv);
+    {
+      const int32_t* table = P.table + b * P.ld_table;
+      auto page_of = [&](int u) {
+        const int k0 = u * kUnit + 16 * warp;
+        return u < u1 && k0 < seen ? __ldg(table + (k0 >> P.shift)) : -1;
+      };
+      auto off_of = [&](int u) { return (u * kUnit + 16 * warp) & ((1 << P.shift) - 1); };
+      Keys<kSteps> A, B;
+      A.load(P, page_of(u0), h, off_of(u0), g, t);
+      int next = page_of(u0 + 1);
+#pragma unroll 1
+      for (int u = u0; u < u1; u += 2) {
+        B.load(P, next, h, off_of(u + 1), g, t);
+        next = page_of(u + 2);
+        R.take(A, u * kUnit + 16 * warp, g);
+        A.load(P, next, h, off_of(u + 2), g, t);
+        next = page_of(u + 3);
+        R.take(B, (u + 1) * kUnit + 16 * warp, g);
+      }
+    }
+
+    // ---- the warps' sums joined
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float z = R.z[i][c];
+        z += __shfl_xor_sync(0xffffffffu, z, 4);
+        z += __shfl_xor_sync(0xffffffffu, z, 8);
+        z += __shfl_xor_sync(0xffffffffu, z, 16);
+        const int row = 8 * i + 2 * t + c;
+        if (g == 0) { S.m[warp][row] = R.m[i][c]; S.z[warp][row] = z; }
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j)
+          *reinterpret_cast<float2*>(&S.o[warp][row][16 * j + 2 * g]) = make_float2(R.o[i][j][c], R.o[i][j][2 + c]);
+      }
+    if (tid < kRowsOf) S.sums[tid] = 0;
+    __syncthreads();
+    const bool whole = u0 == 0 && u1 == sh.units;
+    const long long job_at = start + (long long)job * sh.units;
+    const int w0 = int(((job_at + 1) * workers - 1) / total), w1 = int(((job_at + sh.units) * workers - 1) / total);
+    auto part_of = [&](int w) { return P.partials + (2 * w + (w == w0 ? 1 : 0)) * int64_t(kPart); };
+    float* mine = part_of(blockIdx.x);
+    auto put_row = [&](int row, int d, float a, float b2, float m, float z) {
+      const int r = row0 + row, token = rq.q0 + r / P.group, head = h * P.group + r % P.group;
+      const float inv = z > 0.f ? __fdividef(1.f, z) : z == 0.f ? 0.f : CUDART_NAN_F;
+      const int sum = store_pair(P, token, head, d, a * inv, b2 * inv);
+      if (P.out_row_sum) atomicAdd(&S.sums[row], sum);
+      if (d == 0 && P.lse) P.lse[int64_t(token) * P.heads + head] = z > 0.f ? (m - kLift + log2f(z)) * kLn2 : z == 0.f ? -CUDART_INF_F : CUDART_NAN_F;
+    };
+    for (int e = tid; e < live * (dh / 2); e += kThreads) {
+      const int row = e / (dh / 2), pair = e - row * (dh / 2), pg = pair / kSteps, pj = pair - pg * kSteps;
+      float m = S.m[0][row];
+#pragma unroll
+      for (int w = 1; w < kWarps; ++w) m = fmaxf(m, S.m[w][row]);
+      const float base = m == -CUDART_INF_F ? 0.f : m;
+      float a = 0.f, b2 = 0.f, z = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = ex2(S.m[w][row] - base);
+        const float2 v = *reinterpret_cast<const float2*>(&S.o[w][row][16 * pj + 2 * pg]);
+        a = fmaf(f, v.x, a);
+        b2 = fmaf(f, v.y, b2);
+        z = fmaf(f, S.z[w][row], z);
+      }
+      if (whole) put_row(row, 2 * pair, a, b2, m, z);
+      else {
+        __stcg(reinterpret_cast<float2*>(mine + row * dh + 2 * pair), make_float2(a, b2));
+        if (pair == 0) __stcg(reinterpret_cast<float2*>(mine + kRowsOf * dh + 2 * row), make_float2(m, z));
+      }
+    }
+    bool writes = whole;
+    if (!whole) {
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        const int n = atomicAdd(P.counters + w0, 1);
+        S.last = n == w1 - w0;
+        if (S.last) P.counters[w0] = 0;           // (nobody else counts here any more)
+      }
+      __syncthreads();
+      if (S.last) {
+        __threadfence();
+        writes = true;
+        for (int e = tid; e < live * (dh / 2); e += kThreads) {
+          const int row = e / (dh / 2), pair = e - row * (dh / 2);
+          float m = -CUDART_INF_F, a = 0.f, b2 = 0.f, z = 0.f;
+#pragma unroll 4
+          for (int w = w0; w <= w1; ++w) {
+            const float* p = part_of(w);
+            const float2 mz = __ldcg(reinterpret_cast<const float2*>(p + kRowsOf * dh + 2 * row));
+            const float2 v = __ldcg(reinterpret_cast<const float2*>(p + row * dh + 2 * pair));
+            const float top = fmaxf(m, mz.x), base = top == -CUDART_INF_F ? 0.f : top;
+            const float f = ex2(m - base), f2 = ex2(mz.x - base);
+            a = fmaf(f, a, f2 * v.x);
+            b2 = fmaf(f, b2, f2 * v.y);
+            z = fmaf(f, z, f2 * mz.y);
+            m = top;
+          }
+          put_row(row, 2 * pair, a, b2, m, z);
+        }
+      }
+    }
+    __syncthreads();
+    if (writes && P.out_row_sum && tid < live) atomicAdd(P.out_row_sum + rq.q0 + (row0 + tid) / P.group, S.sums[tid]);
+    at += u1 - u0;
+    __syncthreads();
+  }
+}
+
+// Grid: every SM full, at most a CTA per unit that the bounds of the call allow.
+template <int kSteps, int kTiles, bool kPrecise>
+repq_status plan_of(const AttendParams& P, RowsPlan* plan) {
+  static Residency memo;
+  int per_sm;
+  REPQ_TRY(resident_blocks(memo, cache_rows_kernel<kSteps, kTiles, kPrecise>, kThreads, 0, &per_sm));
+  const int64_t tiles = (int64_t(P.max_q) * P.group + 8 * kTiles - 1) / (8 * kTiles);
+  const int64_t units = int64_t(P.requests) * P.c.kv_heads * tiles * ((int64_t(P.max_kv) + kUnit - 1) / kUnit > 0 ? (int64_t(P.max_kv) + kUnit - 1) / kUnit : 1);
+  const int64_t most = int64_t(sm_count()) * per_sm;
+  plan->row_tiles = kTiles;
+  plan->workers = int(units < most ? units : most);
+  plan->counter_bytes = size_t(round_up(int64_t(plan->workers) * 4, 256));
+  plan->workspace = plan->counter_bytes + size_t(plan->workers) * 2 * (8 * kTiles) * (16 * kSteps + 2) * sizeof(float);
+  return REPQ_OK;
+}
+
+template <int kSteps, int kTiles, bool kPrecise>
+repq_status launch(AttendParams P, void* workspace, cudaStream_t st) {
+  RowsPlan plan;
+  REPQ_TRY((plan_of<kSteps, kTiles, kPrecise>(P, &plan)));
+  P.counters = static_cast<int32_t*>(workspace);
+  P.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + plan.counter_bytes);
+  REPQ_CUDA(launch_chained(cache_rows_kernel<kSteps, kTiles, kPrecise>, dim3(plan.workers), dim3(kThreads), 0, st, P));
+  note_launch();
+  return REPQ_OK;
+}
+
+// One of the forms: a plan, or a launch where `workspace_of` is given.
+template <bool kPrecise, int kTiles>
+repq_status for_width(const AttendParams& P, RowsPlan* plan, void* workspace, cudaStream_t st) {
+  switch (P.c.d_h / 16) {
+#define REPQ_CASE(S)                                                               \
+  case S: return plan ? plan_of<S, kTiles, kPrecise>(P, plan) : launch<S, kTiles, kPrecise>(P, workspace, st);
+    REPQ_CASE(1) REPQ_CASE(2) REPQ_CASE(3) REPQ_CASE(4) REPQ_CASE(5) REPQ_CASE(6) REPQ_CASE(7) REPQ_CASE(8)
+#undef REPQ_CASE
+  }
+  return fail(REPQ_UNSUPPORTED, "repq_cache_attention: d_h %d", P.c.d_h);
+}
+
+repq_status run_bf16_1(const AttendParams& P, RowsPlan* plan, void* workspace, cudaStream_t st);
+repq_status run_bf16_2(const AttendParams& P, RowsPlan* plan, void* workspace, cudaStream_t st);
+repq_status run_f32_1(const AttendParams& P, RowsPlan* plan, void* workspace, cudaStream_t st);
+repq_status run_f32_2(const AttendParams& P, RowsPlan* plan, void* workspace, cudaStream_t st);
+
+}  // namespace rows
+}  // namespace cache
+}  // namespace repq

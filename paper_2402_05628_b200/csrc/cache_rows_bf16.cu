@@ -1,0 +1,23 @@
+// Attention over the 8-bit cache, few rows, bf16 queries (the kernel is in cache_attention_rows.cuh), and the choice of its form.
+#include "cache_attention_rows.cuh"
+
+namespace repq {
+namespace cache {
+namespace rows {
+repq_status run_bf16_1(const AttendParams& P, RowsPlan* plan, void* workspace, cudaStream_t st) { return for_width<false, 1>(P, plan, workspace, st); }
+
+namespace {
+// Eight rows to a job, or sixteen where there are more: keys are then read and converted half as often.
+repq_status run(const AttendParams& P, bool precise, RowsPlan* plan, void* workspace, cudaStream_t st) {
+  const bool two = int64_t(P.max_q) * P.group > 8;
+  if (precise) return two ? run_f32_2(P, plan, workspace, st) : run_f32_1(P, plan, workspace, st);
+  return two ? run_bf16_2(P, plan, workspace, st) : run_bf16_1(P, plan, workspace, st);
+}
+}  // namespace
+}  // namespace rows
+
+repq_status rows_plan(const AttendParams& P, bool precise, RowsPlan* plan) { return rows::run(P, precise, plan, nullptr, nullptr); }
+repq_status launch_rows(AttendParams P, bool precise, void* workspace, cudaStream_t st) { return rows::run(P, precise, nullptr, workspace, st); }
+
+}  // namespace cache
+}  // namespace repq

@@ -1,0 +1,10 @@
+// Attention over the 8-bit cache, few rows, bf16 queries, sixteen rows a job (the kernel is in cache_attention_rows.cuh).
+#include "cache_attention_rows.cuh"
+
+namespace repq {
+namespace cache {
+namespace rows {
+repq_status run_bf16_2(const AttendParams& P, RowsPlan* plan, void* workspace, cudaStream_t st) { return for_width<false, 2>(P, plan, workspace, st); }
+}  // namespace rows
+}  // namespace cache
+}  // namespace repq

@@ -1,0 +1,10 @@
+// Attention over the 8-bit cache, few rows, float32 queries, sixteen rows a job (the kernel is in cache_attention_rows.cuh).
+#include "cache_attention_rows.cuh"
+
+namespace repq {
+namespace cache {
+namespace rows {
+repq_status run_f32_2(const AttendParams& P, RowsPlan* plan, void* workspace, cudaStream_t st) { return for_width<true, 2>(P, plan, workspace, st); }
+}  // namespace rows
+}  // namespace cache
+}  // namespace repq

@@ -1,0 +1,366 @@
+// Log probabilities of given tokens, entropy, rank and the most probable alternatives, one pass over the logits.
+#include <cuda_bf16.h>
+#include <math_constants.h>
+
+#include "f32x2.cuh"
+#include "kernels.h"
+
+namespace repq {
+namespace scoring {
+namespace {
+
+constexpr int kMostTop = 32;
+constexpr int kCand = 256;                        // candidates of a CTA
+constexpr int kMostSplit = 8;                     // CTAs of a row (a cluster)
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct Params {
+  const void* x;
+  int64_t ld;
+  int rows, vocab, top, per;                      // per: elements of a row that a CTA of its cluster takes (a multiple of 8)
+  int vec;                                        // rows start on 16-byte boundaries
+  const int32_t* tokens;
+  float *logprob, *entropy, *top_logprobs;
+  int32_t *rank, *top_ids;
+};
+
+// The order of the tokens of a row: logit descending, then index ascending.  A number that grows with the logit, NaN lowest ...
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t u = __float_as_uint(x + 0.0f);   // (-0 counts as +0)
+  return x != x ? 0u : (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+// ... and one that is larger for whatever comes first.
+__device__ __forceinline__ uint64_t key_of(float x, int i) { return uint64_t(order_of(x)) << 32 | uint32_t(~i); }
+__device__ __forceinline__ int index_of(uint64_t key) { return int(~uint32_t(key)); }
+__device__ __forceinline__ float value_of(uint64_t key) {
+  const uint32_t u = uint32_t(key >> 32);
+  return u == 0u ? CUDART_NAN_F : __uint_as_float((u & 0x80000000u) ? u & 0x7fffffffu : ~u);
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// What a stretch of a row says: m = max x (NaN left out), z = sum 2^(c (x - m)), w = sum 2^(c (x - m)) c (x - m), c = log2 e.
+struct Stats { float m, z, w; };
+__device__ __forceinline__ void move_to(Stats& a, float m) {      // m >= a.m
+  if (a.m == m) return;
+  const float d = fmaxf((a.m - m) * kLog2e, -1e30f);              // (-inf where nothing has been seen: z = w = 0)
+  const float f = ex2(d);
+  a.w = f * fmaf(a.z, d, a.w);
+  a.z *= f;
+  a.m = m;
+}
+__device__ __forceinline__ Stats joined(Stats a, Stats b) {
+  const float m = fmaxf(a.m, b.m);
+  move_to(a, m);
+  move_to(b, m);
+  return {m, a.z + b.z, a.w + b.w};
+}
+
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+  static constexpr int kN = 4;
+  __device__ __forceinline__ static void get(const uint4& r, float (&f)[4]) {
+    f[0] = __uint_as_float(r.x); f[1] = __uint_as_float(r.y); f[2] = __uint_as_float(r.z); f[3] = __uint_as_float(r.w);
+  }
+  __device__ __forceinline__ static float one(const void* p, int64_t i) { return __ldg(static_cast<const float*>(p) + i); }
+};
+template <> struct Vec<__nv_bfloat16> {
+  static constexpr int kN = 8;
+  __device__ __forceinline__ static void get(const uint4& r, float (&f)[8]) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+  }
+  __device__ __forceinline__ static float one(const void* p, int64_t i) { return __bfloat162float(__ldg(static_cast<const __nv_bfloat16*>(p) + i)); }
+};
+
+template <typename T>
+__device__ __forceinline__ uint4 load_vec(const Params& P, const T* row, int e, int end) {
+  constexpr int kN = Vec<T>::kN;
+  if (P.vec && e + kN <= end) return __ldg(reinterpret_cast<const uint4*>(row + e));
+  union { T t[kN]; uint4 r; } u;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) u.t[i] = e + i < end ? row[e + i] : T(-CUDART_INF_F);
+  return u.r;
+}
+
+__device__ __forceinline__ uint32_t cluster_addr(const void* p, int rank) {
+  uint32_t a = uint32_t(__cvta_generic_to_shared(p)), r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void put_remote(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ void put_remote64(uint32_t addr, uint64_t v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+}
+
+// One row per cluster of kSplit CTAs, a stretch of it per CTA.
+// The first pass has the maximum, the sums, the number of tokens ahead of the given one, and every thread's largest element.  The K-th
+// largest of 64 disjoint groups' largest elements bounds the K-th largest element from below, so a second look at the stretch (from
+// cache) picks the few elements above that bound, which are then sorted by counting.
+template <typename T, int kThreads, int kSplit>
+__global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const __grid_constant__ Params P) {
+  constexpr int kN = Vec<T>::kN, kWarps = kThreads / 32, kFly = 4;
+  __shared__ Stats warp_stats[kWarps];
+  __shared__ int warp_ahead[kWarps];
+  __shared__ uint64_t cand[kCand];
+  __shared__ float group_top[64];
+  __shared__ int n_cand;
+  __shared__ float bound;
+  __shared__ Stats all_stats[kSplit];
+  __shared__ int all_ahead[kSplit];
+  __shared__ uint64_t all_top[kSplit][kMostTop];
+  __shared__ float lse_s;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int part = kSplit > 1 ? int(blockIdx.x % kSplit) : 0;
+  const int r = kSplit > 1 ? int(blockIdx.x / kSplit) : int(blockIdx.x);
+  if (kSplit > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // (every CTA of the cluster runs: waited for below)
+  grid_dependency_wait();
+  grid_dependency_trigger();
+  const T* row = static_cast<const T*>(P.x) + r * P.ld;
+  const int begin = min(part * P.per, P.vocab), end = min(begin + P.per, P.vocab);
+  const int token = P.tokens ? __ldg(P.tokens + r) : -1;
+  const bool given = token >= 0 && token < P.vocab;
+  const float xt = given ? Vec<T>::one(row, token) : 0.f;
+
+  Stats s = {-CUDART_INF_F, 0.f, 0.f};
+  int ahead = 0;
+  auto take = [&](const uint4& v, int e) {
+    float f[kN];
+    Vec<T>::get(v, f);
+    float top = f[0];
+#pragma unroll
+    for (int i = 1; i < kN; ++i) top = fmaxf(top, f[i]);
+    if (top > s.m) move_to(s, top);
+    const float base = s.m == -CUDART_INF_F ? 0.f : s.m;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const float d = (f[i] - base) * kLog2e, p = ex2(d);
+      s.z += p;
+      s.w = fmaf(p, fmaxf(d, -1e30f), s.w);       // (0 * -inf)
+      ahead += f[i] > xt ? 1 : 0;
+    }
+    if (given && (e <= token || xt != xt)) {       // equal ones count where they come first, and all numbers come before a NaN
+#pragma unroll
+      for (int i = 0; i < kN; ++i)
+        if (e + i < end) ahead += xt != xt ? (f[i] == f[i] || e + i < token) : (f[i] == xt && e + i < token);
+    }
+  };
+  const int step = kThreads * kN;
+  int e = begin + tid * kN;
+  for (; e + (kFly - 1) * step < end; e += kFly * step) {
+    uint4 v[kFly];
+#pragma unroll
+    for (int i = 0; i < kFly; ++i) v[i] = load_vec(P, row, e + i * step, end);
+#pragma unroll
+    for (int i = 0; i < kFly; ++i) take(v[i], e + i * step);
+  }
+  for (; e < end; e += step) take(load_vec(P, row, e, end), e);
+
+  // ---- the CTA's sums; groups' largest elements
+  const float mine = s.m;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const Stats b = {__shfl_xor_sync(0xffffffffu, s.m, o), __shfl_xor_sync(0xffffffffu, s.z, o), __shfl_xor_sync(0xffffffffu, s.w, o)};
+    s = joined(s, b);
+  }
+  ahead = __reduce_add_sync(0xffffffffu, ahead);
+  if (lane == 0) { warp_stats[warp] = s; warp_ahead[warp] = ahead; }
+  if (tid == 0) n_cand = 0;
+  if (P.top > 0) {
+    constexpr int kGroup = kThreads / 64;          // threads of a group
+    float g = mine;
+#pragma unroll
+    for (int o = kGroup / 2; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
+    if (tid % kGroup == 0) group_top[tid / kGroup] = g;
+  }
+  __syncthreads();
+  if (kSplit > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (tid == 0) {
+    Stats a = warp_stats[0];
+    int n = warp_ahead[0];
+    for (int w = 1; w < kWarps; ++w) { a = joined(a, warp_stats[w]); n += warp_ahead[w]; }
+    if (kSplit == 1) { all_stats[0] = a; all_ahead[0] = n; }
+    else {
+      const uint32_t to = cluster_addr(&all_stats[part], 0), to_n = cluster_addr(&all_ahead[part], 0);
+      put_remote(to, __float_as_uint(a.m));
+      put_remote(to + 4, __float_as_uint(a.z));
+      put_remote(to + 8, __float_as_uint(a.w));
+      put_remote(to_n, uint32_t(n));
+    }
+  }
+  if (P.top > 0) {
+    if (warp == kWarps - 1) {                      // the K-th largest of the 64
+      const float a = group_top[lane], b = group_top[lane + 32];
+      int na = 0, nb = 0;                          // groups ahead of mine, ties by place
+#pragma unroll 8
+      for (int i = 0; i < 64; ++i) {
+        const float x = group_top[i];
+        na += x > a || (x == a && i < lane) ? 1 : 0;
+        nb += x > b || (x == b && i < lane + 32) ? 1 : 0;
+      }
+      if (na == P.top - 1) bound = a;
+      if (nb == P.top - 1) bound = b;
+    }
+    __syncthreads();
+    const float least = bound;
+    if (least > -CUDART_INF_F) {
+      auto pick = [&](const uint4& v, int at) {
+        float f[kN];
+        Vec<T>::get(v, f);
+        float top = f[0];
+#pragma unroll
+        for (int i = 1; i < kN; ++i) top = fmaxf(top, f[i]);
+        if (top >= least) {
+#pragma unroll
+          for (int i = 0; i < kN; ++i)
+            if (f[i] >= least && at + i < end) {
+              const int n = atomicAdd(&n_cand, 1);
+              if (n < kCand) cand[n] = key_of(f[i], at + i);
+            }
+        }
+      };
+      if (mine >= least) {                         // (a thread whose own largest is below has none)
+        for (int at = begin + tid * kN; at < end; at += step) pick(load_vec(P, row, at, end), at);
+      }
+      __syncthreads();
+    }
+    int n = n_cand;
+    uint64_t* tops = all_top[0];
+    if (least == -CUDART_INF_F || n > kCand) {
+      // Rows of few finite logits or of many equal ones: one after the other, the first behind the one before.
+      __shared__ uint64_t warp_key[kWarps];
+      uint64_t last = ~uint64_t(0);
+      for (int k = 0; k < P.top; ++k) {
+        uint64_t best = 0;
+        for (int i = begin + tid; i < end; i += kThreads) {
+          const uint64_t key = key_of(Vec<T>::one(row, i), i);
+          if (key < last && key > best) best = key;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+          const uint64_t b = __shfl_xor_sync(0xffffffffu, best, o);
+          best = b > best ? b : best;
+        }
+        if (lane == 0) warp_key[warp] = best;
+        __syncthreads();
+        for (int w = 0; w < kWarps; ++w) best = warp_key[w] > best ? warp_key[w] : best;
+        if (tid == 0) cand[k] = best;              // (0: the stretch has no more)
+        last = best;
+        __syncthreads();
+      }
+      n = P.top;
+    }
+    // sorted by counting; the first `top` go to the row's first CTA
+    for (int i = tid; i < n; i += kThreads) {
+      const uint64_t key = cand[i];
+      int before = 0;
+      for (int j = 0; j < n; ++j) before += cand[j] > key || (cand[j] == key && j < i) ? 1 : 0;
+      if (before < P.top) {
+        if (kSplit == 1) tops[before] = key;
+        else put_remote64(cluster_addr(&all_top[part][before], 0), key);
+      }
+    }
+  }
+  if (kSplit > 1) cluster_barrier();
+  else __syncthreads();
+  if (part != 0) return;
+
+  // ---- the row
+  if (tid == 0) {
+    Stats a = all_stats[0];
+    int n = all_ahead[0];
+#pragma unroll
+    for (int i = 1; i < kSplit; ++i) { a = joined(a, all_stats[i]); n += all_ahead[i]; }
+    const bool empty = a.m == -CUDART_INF_F && a.z == 0.f;
+    const float log2z = log2f(a.z);
+    const float lse = empty ? CUDART_INF_F : a.m + log2z * kLn2;
+    lse_s = lse;
+    if (P.entropy) P.entropy[r] = empty ? 0.f : kLn2 * (log2z - a.w / a.z);
+    if (P.logprob) P.logprob[r] = !given ? 0.f : empty ? -CUDART_INF_F : (xt - a.m) - log2z * kLn2;
+    if (P.rank) P.rank[r] = given ? n + 1 : 0;
+    warp_stats[0] = {a.m, log2z * kLn2, empty ? 1.f : 0.f};
+  }
+  if (P.top > 0) {
+    __syncthreads();
+    const Stats a = warp_stats[0];
+    auto put = [&](int k, uint64_t key) {
+      P.top_ids[r * int64_t(P.top) + k] = index_of(key);
+      P.top_logprobs[r * int64_t(P.top) + k] = a.w != 0.f ? -CUDART_INF_F : (value_of(key) - a.m) - a.z;
+    };
+    if (kSplit == 1) {
+      if (tid < P.top) put(tid, all_top[0][tid]);
+    } else {
+      for (int i = tid; i < kSplit * P.top; i += kThreads) {
+        const int ip = i / P.top, ik = i - ip * P.top;
+        const uint64_t key = all_top[ip][ik];
+        int before = ik;                           // a part's own are in order
+#pragma unroll
+        for (int p = 0; p < kSplit; ++p)
+          if (p != ip)
+            for (int k = 0; k < P.top && (all_top[p][k] > key || (all_top[p][k] == key && p < ip)); ++k) ++before;
+        if (before < P.top) put(before, key);
+      }
+    }
+  }
+}
+
+template <typename T, int kThreads, int kSplit>
+repq_status launch(const Params& P, cudaStream_t st) {
+  REPQ_CUDA(launch_chained_cluster(token_logprobs_kernel<T, kThreads, kSplit>, dim3(unsigned(P.rows) * kSplit), dim3(kThreads), 0, st, kSplit, P));
+  note_launch();
+  return REPQ_OK;
+}
+
+template <typename T>
+repq_status choose(Params& P, cudaStream_t st) {
+  // a row to a CTA where that fills the SMs, or to a cluster of up to eight
+  int split = 1;
+  while (split < kMostSplit && P.rows * split * 2 <= 2 * sm_count() && P.vocab / (split * 2) >= 1024) split *= 2;
+  P.per = int(round_up((P.vocab + split - 1) / split, 8));
+  switch (split) {
+    case 1: return launch<T, 256, 1>(P, st);
+    case 2: return launch<T, 256, 2>(P, st);
+    case 4: return launch<T, 256, 4>(P, st);
+    default: return launch<T, 256, 8>(P, st);
+  }
+}
+
+}  // namespace
+}  // namespace scoring
+}  // namespace repq
+
+using namespace repq;
+
+extern "C" repq_status repq_token_logprobs(const repq_token_logprobs_desc* d, void* stream) {
+  REPQ_REQUIRE(d != nullptr, REPQ_INVALID_ARG, "repq_token_logprobs: NULL descriptor");
+  REPQ_REQUIRE(d->rows >= 0 && d->vocab > 0, REPQ_INVALID_ARG, "repq_token_logprobs: rows %d, vocab %d", d->rows, d->vocab);
+  REPQ_REQUIRE(d->dtype == REPQ_F32 || d->dtype == REPQ_BF16, REPQ_INVALID_ARG, "repq_token_logprobs: dtype %d", d->dtype);
+  REPQ_REQUIRE(d->top >= 0 && d->top <= scoring::kMostTop && d->top <= d->vocab, REPQ_UNSUPPORTED,
+               "repq_token_logprobs: top %d is not in 0..min(vocab, %d)", d->top, scoring::kMostTop);
+  if (d->rows == 0) return REPQ_OK;
+  REPQ_REQUIRE(d->rows <= (1 << 27), REPQ_UNSUPPORTED, "repq_token_logprobs: too many rows");
+  REPQ_REQUIRE(d->vocab <= (1 << 30), REPQ_UNSUPPORTED, "repq_token_logprobs: vocab %d", d->vocab);
+  REPQ_REQUIRE(d->logits, REPQ_INVALID_ARG, "repq_token_logprobs: NULL logits");
+  REPQ_REQUIRE(d->ld >= d->vocab || d->rows == 1, REPQ_INVALID_ARG, "repq_token_logprobs: ld is smaller than vocab");
+  REPQ_REQUIRE(d->tokens || (!d->logprob && !d->rank), REPQ_INVALID_ARG, "repq_token_logprobs: logprob and rank need tokens");
+  REPQ_REQUIRE(d->top == 0 || (d->top_ids && d->top_logprobs), REPQ_INVALID_ARG, "repq_token_logprobs: NULL top outputs");
+  const int unit = d->dtype == REPQ_F32 ? 4 : 2;
+  REPQ_REQUIRE(aligned(d->logits, unit), REPQ_ALIGNMENT, "repq_token_logprobs: logits are not aligned to their type");
+  scoring::Params P;
+  P.x = d->logits; P.ld = d->ld; P.rows = d->rows; P.vocab = d->vocab; P.top = d->top;
+  P.vec = aligned(d->logits, 16) && (d->ld * unit) % 16 == 0;
+  P.tokens = d->tokens; P.logprob = d->logprob; P.entropy = d->entropy; P.rank = d->rank;
+  P.top_ids = d->top_ids; P.top_logprobs = d->top_logprobs;
+  return d->dtype == REPQ_F32 ? scoring::choose<float>(P, static_cast<cudaStream_t>(stream))
+                              : scoring::choose<__nv_bfloat16>(P, static_cast<cudaStream_t>(stream));
+}
