@@ -50,7 +50,46 @@ repq_status prepare(const repq_cache_attention_desc* d, AttendParams* out, bool*
 
 bool nothing(const AttendParams& P) { return P.requests == 0 || P.max_q == 0; }
 
+// Which kernels a call takes.  Requests of up to kFewRows rows go to the kernel for few rows, others to the one for chunks; float32
+// queries always to the former.  Lengths are known on the device only: where the bounds allow both kinds both kernels run, each passes
+// over the other's requests.
+constexpr int kFewRows = 48;
+struct Route { bool rows, chunks; int few; RowsPlan rp; ChunksPlan cp; size_t rows_bytes, workspace; };
+repq_status route_of(AttendParams& P, bool precise, Route* out) {
+  Route r = {};
+  const int64_t most = int64_t(P.max_q) * P.group;
+  if (precise || most <= kFewRows) { r.rows = true; r.few = INT32_MAX; }
+  else {
+    // as many tokens as max_q_len allows: every request is a chunk
+    r.chunks = true;
+    r.rows = int64_t(P.tokens) != int64_t(P.requests) * P.max_q;
+    r.few = r.rows ? kFewRows : 0;
+  }
+  P.few = r.few;
+  if (r.rows) {
+    REPQ_TRY(rows_plan(P, precise, &r.rp));
+    r.rows_bytes = size_t(round_up(int64_t(r.rp.workspace), 256));
+    r.workspace = r.rows_bytes;
+  }
+  if (r.chunks) {
+    r.cp = chunks_plan(P);
+    r.workspace += r.cp.workspace;
+  }
+  *out = r;
+  return REPQ_OK;
+}
+
 }  // namespace
+
+ChunksPlan chunks_plan(const AttendParams& P) {
+  ChunksPlan plan;
+  plan.ctas = sm_count();
+  // two counters for the items, two per item that is cut along the keys (at most half as many items as CTAs), and a part per CTA then
+  plan.counter_bytes = size_t(round_up(4 * (2 + int64_t(plan.ctas)), 256));
+  plan.workspace = plan.counter_bytes + size_t(plan.ctas) * 256 * (P.c.d_h + 2) * sizeof(float);
+  return plan;
+}
+
 }  // namespace cache
 }  // namespace repq
 
@@ -63,9 +102,9 @@ extern "C" repq_status repq_cache_attention_workspace_bytes(const repq_cache_att
   bool precise;
   REPQ_TRY(cache::prepare(d, &P, &precise));
   if (cache::nothing(P)) return REPQ_OK;
-  cache::RowsPlan plan;
-  REPQ_TRY(cache::rows_plan(P, precise, &plan));
-  *bytes = plan.workspace;
+  cache::Route route;
+  REPQ_TRY(cache::route_of(P, precise, &route));
+  *bytes = route.workspace;
   return REPQ_OK;
 }
 
@@ -81,10 +120,16 @@ extern "C" repq_status repq_cache_attention(const repq_cache_attention_desc* d, 
   const int64_t out_unit = d->out_kind == REPQ_OUT_F32 ? 4 : d->out_kind == REPQ_OUT_BF16 ? 2 : 1, out_align = d->out_kind == REPQ_OUT_CODES ? 4 : 16;
   REPQ_REQUIRE(aligned(d->out, out_align) && (d->ldo | d->o_stride_head) * out_unit % out_align == 0, REPQ_ALIGNMENT,
                "repq_cache_attention: rows of out must be %d-byte aligned", int(out_align));
-  cache::RowsPlan plan;
-  REPQ_TRY(cache::rows_plan(P, precise, &plan));
-  REPQ_REQUIRE(plan.workspace == 0 || (workspace && workspace_bytes >= plan.workspace), REPQ_WORKSPACE_TOO_SMALL,
-               "repq_cache_attention: workspace of %zu bytes, %zu are needed", workspace_bytes, plan.workspace);
+  cache::Route route;
+  REPQ_TRY(cache::route_of(P, precise, &route));
+  REPQ_REQUIRE(workspace && workspace_bytes >= route.workspace, REPQ_WORKSPACE_TOO_SMALL,
+               "repq_cache_attention: workspace of %zu bytes, %zu are needed", workspace_bytes, route.workspace);
   REPQ_REQUIRE(aligned(workspace, 16), REPQ_ALIGNMENT, "repq_cache_attention: workspace must be 16-byte aligned");
-  return cache::launch_rows(P, precise, workspace, static_cast<cudaStream_t>(stream));
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (route.chunks) {
+    uint8_t* w = static_cast<uint8_t*>(workspace) + route.rows_bytes;
+    REPQ_TRY(P.c.d_h <= 64 ? cache::chunks::run_narrow(P, route.cp, route.few, w, st) : cache::chunks::run_wide(P, route.cp, route.few, w, st));
+  }
+  if (route.rows) REPQ_TRY(cache::launch_rows(P, precise, workspace, st));
+  return REPQ_OK;
 }

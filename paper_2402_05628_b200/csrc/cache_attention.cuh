@@ -15,6 +15,7 @@ struct AttendParams {
   int shift;                             // log2 block_size
   int requests, tokens, heads, group;    // group: query heads of a key / value head
   int max_q, max_kv;
+  int few;                               // rows (tokens x group) of a request up to which the kernel for few rows takes it
   const void* q; int64_t q_st, q_sh;
   const int32_t* table; int64_t ld_table; int table_width;
   const int32_t* kv_lens; const int32_t* cu_q;
@@ -81,10 +82,19 @@ __device__ __forceinline__ int store_pair(const AttendParams& P, int token, int 
   return ca + cb;
 }
 
-// The kernel for a few rows per key / value head (cache_attention_rows.cu): how it would be launched, and the launch.
-struct RowsPlan { int row_tiles, workers; size_t counter_bytes, workspace; };
+// The kernel for few rows per key / value head (cache_attention_rows.cuh): requests of at most P.few rows.  How it would be launched, and
+// the launch, whose workspace begins with counters that are zero between calls.
+struct RowsPlan { int workers; size_t counter_bytes, workspace; };
 repq_status rows_plan(const AttendParams& P, bool precise, RowsPlan* plan);
 repq_status launch_rows(AttendParams P, bool precise, void* workspace, cudaStream_t st);
+
+// The kernel for many rows (cache_attention_chunks.cuh): requests of more than `few` rows, bf16 queries.
+struct ChunksPlan { int ctas; size_t counter_bytes, workspace; };
+ChunksPlan chunks_plan(const AttendParams& P);
+namespace chunks {
+repq_status run_narrow(const AttendParams& A, const ChunksPlan& plan, int few, void* workspace, cudaStream_t st);
+repq_status run_wide(const AttendParams& A, const ChunksPlan& plan, int few, void* workspace, cudaStream_t st);
+}  // namespace chunks
 
 }  // namespace cache
 }  // namespace repq

@@ -258,7 +258,8 @@ struct Shared {
 struct Share { int tiles, units; };
 __device__ __forceinline__ Share share_of(const AttendParams& P, const Request& rq, int tile_rows) {
   Share s;
-  s.tiles = (rq.q_len * P.group + tile_rows - 1) / tile_rows;
+  const int rows = rq.q_len * P.group;
+  s.tiles = rows > P.few ? 0 : (rows + tile_rows - 1) / tile_rows;
   s.units = max((min(rq.kv, P.max_kv) + kUnit - 1) / kUnit, 1);
   return s;
 }
@@ -442,10 +443,10 @@ repq_status plan_of(const AttendParams& P, RowsPlan* plan) {
   static Residency memo;
   int per_sm;
   REPQ_TRY(resident_blocks(memo, cache_rows_kernel<kSteps, kTiles, kPrecise>, kThreads, 0, &per_sm));
-  const int64_t tiles = (int64_t(P.max_q) * P.group + 8 * kTiles - 1) / (8 * kTiles);
+  const int64_t rows = int64_t(P.max_q) * P.group;
+  const int64_t tiles = ((rows < P.few ? rows : P.few) + 8 * kTiles - 1) / (8 * kTiles);
   const int64_t units = int64_t(P.requests) * P.c.kv_heads * tiles * ((int64_t(P.max_kv) + kUnit - 1) / kUnit > 0 ? (int64_t(P.max_kv) + kUnit - 1) / kUnit : 1);
   const int64_t most = int64_t(sm_count()) * per_sm;
-  plan->row_tiles = kTiles;
   plan->workers = int(units < most ? units : most);
   plan->counter_bytes = size_t(round_up(int64_t(plan->workers) * 4, 256));
   plan->workspace = plan->counter_bytes + size_t(plan->workers) * 2 * (8 * kTiles) * (16 * kSteps + 2) * sizeof(float);

@@ -1,0 +1,18 @@
+// Attention over the 8-bit cache, chunks of prompts (the kernel is in cache_attention_chunks.cuh), heads of 16 to 64 channels.
+#include "cache_attention_chunks.cuh"
+
+namespace repq {
+namespace cache {
+namespace chunks {
+repq_status run_narrow(const AttendParams& A, const ChunksPlan& plan, int few, void* workspace, cudaStream_t st) {
+  switch (A.c.d_h / 16) {
+    case 1: return launch<1>(A, plan, few, workspace, st);
+    case 2: return launch<2>(A, plan, few, workspace, st);
+    case 3: return launch<3>(A, plan, few, workspace, st);
+    case 4: return launch<4>(A, plan, few, workspace, st);
+  }
+  return fail(REPQ_UNSUPPORTED, "repq_cache_attention: d_h %d", A.c.d_h);
+}
+}  // namespace chunks
+}  // namespace cache
+}  // namespace repq

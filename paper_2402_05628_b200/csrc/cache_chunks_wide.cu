@@ -1,0 +1,18 @@
+// Attention over the 8-bit cache, chunks of prompts (the kernel is in cache_attention_chunks.cuh), heads of 80 to 128 channels.
+#include "cache_attention_chunks.cuh"
+
+namespace repq {
+namespace cache {
+namespace chunks {
+repq_status run_wide(const AttendParams& A, const ChunksPlan& plan, int few, void* workspace, cudaStream_t st) {
+  switch (A.c.d_h / 16) {
+    case 5: return launch<5>(A, plan, few, workspace, st);
+    case 6: return launch<6>(A, plan, few, workspace, st);
+    case 7: return launch<7>(A, plan, few, workspace, st);
+    case 8: return launch<8>(A, plan, few, workspace, st);
+  }
+  return fail(REPQ_UNSUPPORTED, "repq_cache_attention: d_h %d", A.c.d_h);
+}
+}  // namespace chunks
+}  // namespace cache
+}  // namespace repq

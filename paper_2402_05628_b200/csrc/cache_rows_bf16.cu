@@ -9,7 +9,8 @@ repq_status run_bf16_1(const AttendParams& P, RowsPlan* plan, void* workspace, c
 namespace {
 // Eight rows to a job, or sixteen where there are more: keys are then read and converted half as often.
 repq_status run(const AttendParams& P, bool precise, RowsPlan* plan, void* workspace, cudaStream_t st) {
-  const bool two = int64_t(P.max_q) * P.group > 8;
+  const int64_t most = int64_t(P.max_q) * P.group;
+  const bool two = (most < P.few ? most : P.few) > 8;
   if (precise) return two ? run_f32_2(P, plan, workspace, st) : run_f32_1(P, plan, workspace, st);
   return two ? run_bf16_2(P, plan, workspace, st) : run_bf16_1(P, plan, workspace, st);
 }

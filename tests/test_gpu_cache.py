@@ -234,9 +234,9 @@ class Case:
         self.cu = np.concatenate([[0], np.cumsum(self.q)])
         self.act, self.heads, self.alpha = act, heads, 1.0 / np.sqrt(dh)
 
-    def reference(self, max_kv=None):
+    def reference(self, max_kv=None, chunks=False):
         """(out, lse, a bound on each element's error but for the output's rounding): weights of 11 bits and scores of float32, or 22 bits."""
-        out, lse, tol = np.zeros(self.x.shape), np.full(self.x.shape[:2], -np.inf), np.zeros(self.x.shape)
+        out, lse, tol, floor = np.zeros(self.x.shape), np.full(self.x.shape[:2], -np.inf), np.zeros(self.x.shape), np.zeros(self.x.shape)
         for b in range(len(self.kv)):
             L = int(self.kv[b]) if max_kv is None else min(int(self.kv[b]), max_kv)
             pages = self.table[b, :-(-L // self.bs)]
@@ -261,7 +261,10 @@ class Case:
                     terms = (self.alpha * np.abs(k) @ np.abs(self.x[r, h])).max()    # what a score is made of
                     wt = 2.0 ** -11 if self.act == "bf16" else 2.0 ** -21
                     tol[r, h] = size * (wt + 2.0 ** -20 * (4 + terms + abs(m)))
-        return out, lse, tol
+                    # chunks: weights under 2^-21 of the largest are multiples of 2^-31 of it at least
+                    c = np.maximum(np.abs(v).max(1, initial=0), 1e-300)
+                    floor[r, h] = 2.0 ** -32 * len(e) * 128 * (e * c / 64).max() / e.sum()
+        return out, lse, tol + floor if chunks else tol
 
     def run(self, B, out=None, lse=None, max_q=None, max_kv=None, workspace=None, stream=None, **kw):
         import torch
@@ -278,11 +281,11 @@ class Case:
                                lse=lse, stream=stream, **kw)
         return out
 
-    def check(self, B, **kw):
+    def check(self, B, chunks=False, **kw):
         import torch
         lse = torch.full(self.gx.shape[:2], 7.0, device="cuda:0")
         got = self.run(B, lse=lse, **kw).float().cpu().numpy().astype(np.float64)
-        ref, ref_lse, tol = self.reference(kw.get("max_kv"))
+        ref, ref_lse, tol = self.reference(kw.get("max_kv"), chunks)
         u = 2.0 ** -8 if self.act == "bf16" else 2.0 ** -24
         assert np.isfinite(got).all()
         worst = np.abs(got - ref) - (tol + u * np.abs(ref) + 1e-12)
@@ -322,6 +325,44 @@ def test_attention_long_axis_split_over_the_chip(B, act):
 def test_attention_prompts(B, act):
     Case([300, 129, 128, 1], [300, 129, 1, 1], 4, 2, 128, 32, act, seed=6).check(B)
     Case([700, 450], [200, 333], 3, 3, 64, 16, act, seed=7).check(B)
+
+
+@pytest.mark.parametrize("dh", [16, 32, 48, 64, 80, 96, 112, 128])
+def test_attention_chunk_widths(B, dh):
+    Case([150, 260], [150, 130], 4, 2, dh, 16, seed=dh).check(B)
+
+
+@pytest.mark.parametrize("kv,q,heads,kv_heads,dh,bs", [
+    ([49], [49], 1, 1, 64, 16),                              # a few rows more than the kernel for few rows takes
+    ([3000], [60], 2, 1, 128, 64),                           # one item, cut along the keys over all SMs
+    ([700, 0, 1000, 64], [257, 0, 100, 64], 6, 2, 64, 32),   # groups of three: rows of a token in two tiles; requests of nothing
+    ([900, 333, 5000, 2, 640], [200, 1, 1, 2, 129], 10, 2, 128, 16),   # chunks and single tokens in one call, groups of five
+    ([130, 140], [140, 129], 2, 2, 128, 128),                # more queries than tokens: the first rows see nothing
+    ([256] * 90, [64] * 90, 4, 4, 64, 16),                   # more items than SMs
+    ([4000, 100], [1000, 100], 4, 1, 80, 64),
+])
+def test_attention_chunks(B, kv, q, heads, kv_heads, dh, bs):
+    Case(kv, q, heads, kv_heads, dh, bs, seed=sum(q)).check(B)
+
+
+def test_attention_chunks_rising_maxima(B):
+    """Keys that matter more the later they come, by far: the running maximum moves within steps and between them."""
+    c = Case([600], [200], 2, 2, 64, 32, seed=21)
+    c.scales[0, c.table[0, :19], :] = (np.exp(0.35 * np.arange(19)) / 200.0)[:, None]
+    c.check(B, chunks=True)
+    d = Case([600], [200], 2, 2, 64, 32, seed=22)
+    d.scales[1, d.table[0, :19], :] = (2.0 ** np.arange(-9, 10))[:, None]
+    d.check(B, chunks=True)
+
+
+def test_attention_chunks_repeat_bit_for_bit(B):
+    import torch
+    c = Case([3000, 50, 800], [300, 50, 1], 2, 1, 128, 64, seed=23)
+    ws = torch.zeros(64 << 20, dtype=torch.uint8, device="cuda:0")
+    first = c.run(B, workspace=ws)
+    for _ in range(5):
+        assert torch.equal(c.run(B, workspace=ws), first)
+    assert B.repq_device_status() == 0
 
 
 def test_attention_scales_of_every_size(B):
