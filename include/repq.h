@@ -443,7 +443,7 @@ repq_status repq_block_forward_host(const repq_block_desc* d, const repq_block_p
  * block_size x d_h codes and one scale each for K and V,
  *     value = scale[block, head] * (code - 128),   codes in 1..255   (Eq. 5 with z = 128).
  * Token `slot` = block * block_size + offset.  A request's tokens lie in the blocks its row of the block table names,
- * in order.  The caller owns the memory; a block needs no clearing before its first use.
+ * in order.  The caller owns the memory (less than 64 GiB for K and as much for V); a block needs no clearing before its first use.
  * ---------------------------------------------------------------------------------------------- */
 typedef struct repq_cache {
   uint8_t* k_codes;                     /* [device] [num_blocks][kv_heads][block_size][d_h], dense, 16-byte aligned */

@@ -15,6 +15,7 @@ repq_status check(const repq_cache& c, const char* who) {
   REPQ_REQUIRE(c.d_h >= 16 && c.d_h <= 128 && c.d_h % 16 == 0, REPQ_UNSUPPORTED, "%s: d_h %d is not a multiple of 16 up to 128", who, c.d_h);
   REPQ_REQUIRE(int64_t(c.num_blocks) * c.block_size <= INT32_MAX, REPQ_UNSUPPORTED, "%s: slots of the cache pass 32 bits", who);
   REPQ_REQUIRE(int64_t(c.num_blocks) * c.kv_heads <= INT32_MAX, REPQ_UNSUPPORTED, "%s: scales of the cache pass 32 bits", who);
+  REPQ_REQUIRE(int64_t(c.num_blocks) * c.kv_heads * c.block_size * c.d_h < (int64_t(1) << 36), REPQ_UNSUPPORTED, "%s: K or V codes of 64 GiB", who);
   REPQ_REQUIRE(aligned(c.k_codes, 16) && aligned(c.v_codes, 16) && aligned(c.k_scale, 4) && aligned(c.v_scale, 4), REPQ_ALIGNMENT,
                "%s: cache codes must be 16-byte aligned", who);
   return REPQ_OK;

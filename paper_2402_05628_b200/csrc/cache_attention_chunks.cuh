@@ -1,13 +1,12 @@
 // Attention over the 8-bit cache for chunks of prompts: many rows per key / value head, on tcgen05.
 //
 // A CTA takes 256 rows of one key / value head of a request (token x group) as two tiles of 128, and walks the keys they see in steps
-// of 128.  Four warps turn the codes of a step into f16 tiles of shared memory (code - 128 is exact), K as it comes, V as the MN-major
-// operand of the same layout.  Per tile S = Q K^T goes to 128 columns of tensor memory; a thread per row forms weights 16
-// columns at a time and writes them, f16, over columns it has read, from where O += P V takes them.  The two tiles alternate: one's
-// softmax runs under the other's MMAs.
+// of 128.  Four warps turn the codes of a step into tiles of shared memory (code - 128 is exact in either type): K in bf16, as the queries
+// are, V in f16 as the MN-major operand of the same layout.  Per tile S = Q K^T goes to 128 columns of tensor memory; a thread per row
+// forms weights 32 columns at a time and writes them, f16, over columns it has read, from where O += P V takes them.  The two
+// tiles alternate: one's softmax runs under the other's MMAs.
 //
-// With x = S alpha k_scale log2 e (queries scaled per row to f16's range by a power of two) and lv = log2 v_scale, both per
-// 16 keys, weights are w = 2^(x + lv - m + 7): the value scales go into the exponent, so no product per key is spent on them, and
+// With x = S alpha k_scale log2 e and lv = log2 v_scale, both per 16 keys, weights are w = 2^(x + lv - m + 7): the value scales go into the exponent, so no product per key is spent on them, and
 // the sum is Z = sum w / v_scale, a product per 16 keys.  m follows the largest x + lv of the row at a distance of up to 8, so w
 // is at most 2^15 and the accumulator is rescaled rarely; weights have 11 bits down to 2^-21 of the largest.
 //
@@ -16,6 +15,8 @@
 // Roles: two groups of four softmax warps, four conversion warps, one warp that issues MMAs, one that fetches items.  Every wait is
 // bounded; when one runs out all roles leave, MMAs in flight are drained and tensor memory is freed.
 #pragma once
+#include <type_traits>
+
 #include "cache_attention.cuh"
 #include "f32x2.cuh"
 #include "tc_ptx.cuh"
@@ -49,27 +50,55 @@ struct Shared {
   alignas(1024) uint8_t q[2][kTile];
   alignas(1024) uint8_t k[2][kTile];
   alignas(1024) uint8_t v[2][kTile];
+  alignas(16) uint8_t stage[kSoftWarps][32 * 128];                       // output rows on their way: 128 bytes of a warp's 32 rows
   float4 scale[4][8];                    // per step (four in turn) and 16 keys: k_scale, log2 v_scale, 1 / v_scale
   Item item[2];
-  long long first[kThreads + 1];
+  int first[kThreads + 1];               // items before a thread's requests
   int last[2];
-  alignas(8) uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], p_full[2], pv_done[2], o_empty[2], item_full[2],
-      item_empty[2], done;
+  alignas(8) uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], p_full[2][2], pv_half[2], pv_done[2], o_empty[2], item_full[2],
+      item_empty[2], ask, done;
   uint32_t tmem_base;
   volatile int abort;
 };
 
+// The code that runs every step has to stay small: four roles share an SM's instruction caches, and a form of 148 KB spent a third of its
+// issues waiting for instructions (a cold stretch costs some 15 cycles an instruction).  What is rare stands apart.
 __device__ __forceinline__ bool wait_for(uint64_t& bar, uint32_t parity, volatile int* abort, int code, int32_t* status) {
   return tc::mbar_wait<false>(smem_u32(&bar), parity & 1u, abort, code, status);
 }
 
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr) : "memory");
+}
+// (the registers count as written by the wait: the compiler can neither read nor move them while the load is in flight)
+__device__ __forceinline__ void tmem_ld_wait32(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                 "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                 "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29])
+               :: "memory");
+  asm volatile("" : "+r"(r[30]), "+r"(r[31]));
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
+// Two codes as bf16: 0x4300 | (c & 127) is 128 + c mod 128, from which 256 goes, or 128 where c has its top bit; both exact.
+__device__ __forceinline__ uint32_t bf16_codes(uint32_t w, uint32_t bytes) {
+  const uint32_t t = __byte_perm(w, 0u, bytes), a = (t & 0x007f007fu) | 0x43004300u, b = (t & 0x00800080u) ^ 0xc380c380u;
+  uint32_t d;
+  asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
 
@@ -84,25 +113,101 @@ __device__ __forceinline__ uint32_t piece_at(int r, int c) {
   return uint32_t(c >> 3) * (128u * 128u) + uint32_t(r) * 128u + (uint32_t((c ^ r) & 7) << 4);
 }
 
-// 16 neighbouring values of an output row.
-__device__ __forceinline__ int store16(const AttendParams& P, int token, int head, int d, const float (&v)[16]) {
-  const int64_t at = token * P.ldo + head * P.o_sh;
-  if (P.out_kind == REPQ_OUT_BF16) {
-    uint4* o = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(P.out) + at + d);
-    uint32_t w[8];
+// Weights of blocks [b0, b1) of 32 keys and `o_blocks` blocks of 16 accumulator columns of the warp's rows, times f.
+static __device__ __noinline__ void bring_down(uint32_t t_w, int b0, int b1, uint32_t t_o, int o_blocks, float f) {
+  const __half2 f2 = __float2half2_rn(f);
+#pragma unroll 1
+  for (int b = b0; b < b1; ++b) {
+    uint32_t w[16];
+    tmem_ld16(t_w + 16u * b, w);
+    tmem_ld_wait(w);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&h);
-    }
-    o[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    o[1] = make_uint4(w[4], w[5], w[6], w[7]);
-    return 0;
+    for (int e = 0; e < 16; ++e) w[e] = bits_of(__hmul2(half2_of(w[e]), f2));
+    tmem_st16(t_w + 16u * b, w);
   }
-  int sum = 0;
+#pragma unroll 1
+  for (int b = 0; b < o_blocks; ++b) {
+    uint32_t w[16];
+    tmem_ld16(t_o + 16u * b, w);
+    tmem_ld_wait(w);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sum += store_pair(P, token, head, d + 2 * i, v[2 * i], v[2 * i + 1]);
-  return sum;
+    for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * f);
+    tmem_st16(t_o + 16u * b, w);
+  }
+  tmem_st_wait();
+}
+
+// A tile's part of an item that is cut along the keys: accumulators, m and Z of its rows (a row per thread).
+template <int kSteps>
+__device__ __noinline__ void put_part(float* part, int r, uint32_t t_o, bool any, float m, float z) {
+  if (any) {
+#pragma unroll 1
+    for (int b = 0; b < kSteps; ++b) {
+      uint32_t w[16];
+      tmem_ld16(t_o + 16u * b, w);
+      tmem_ld_wait(w);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        __stcg(reinterpret_cast<uint4*>(part) + (4 * b + e) * kTileRows + r, make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]));
+    }
+  }
+  __stcg(reinterpret_cast<float2*>(part + kTileRows * 16 * kSteps) + r, make_float2(any ? m : -CUDART_INF_F, any ? z : 0.f));
+  __threadfence();
+}
+
+// The output of a row that does not leave by whole bf16 rows: parts joined in order, or (one part) the accumulators; any kind of output.
+struct OutRow { int token, head; bool in; };
+template <int kSteps>
+__device__ __noinline__ float2 put_row(const AttendParams& A, OutRow row, int r, uint32_t t_o, bool any, float m, float z, const float* parts0, int parts) {
+  constexpr int dh = 16 * kSteps, kPart = kTileRows * (dh + 2);
+  if (parts > 1) {
+    m = -CUDART_INF_F;
+    z = 0.f;
+    for (int p = 0; p < parts; ++p) m = fmaxf(m, __ldcg(reinterpret_cast<const float2*>(parts0 + int64_t(2 * p) * kPart + kTileRows * dh) + r).x);
+    for (int p = 0; p < parts; ++p) {
+      const float2 mz = __ldcg(reinterpret_cast<const float2*>(parts0 + int64_t(2 * p) * kPart + kTileRows * dh) + r);
+      if (mz.x > -CUDART_INF_F) z = fmaf(ex2(mz.x - m), mz.y, z);
+    }
+  }
+  const float inv = z > 0.f ? __fdividef(1.f, z) : z == 0.f ? 0.f : CUDART_NAN_F;
+  int sum = 0;
+#pragma unroll 1
+  for (int b = 0; b < kSteps; ++b) {
+    float v[16];
+    if (parts == 1) {
+      uint32_t w[16] = {};
+      if (any) {
+        tmem_ld16(t_o + 16u * b, w);
+        tmem_ld_wait(w);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(w[e]) * inv;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = 0.f;
+#pragma unroll 1
+      for (int p = 0; p < parts; ++p) {
+        const float* pp = parts0 + int64_t(2 * p) * kPart;
+        const float mp = __ldcg(reinterpret_cast<const float2*>(pp + kTileRows * dh) + r).x;
+        if (mp == -CUDART_INF_F) continue;                // (saw nothing, wrote nothing)
+        const float f = ex2(mp - m) * inv;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float4 w = __ldcg(reinterpret_cast<const float4*>(pp) + (4 * b + e) * kTileRows + r);
+          v[4 * e] = fmaf(f, w.x, v[4 * e]);
+          v[4 * e + 1] = fmaf(f, w.y, v[4 * e + 1]);
+          v[4 * e + 2] = fmaf(f, w.z, v[4 * e + 2]);
+          v[4 * e + 3] = fmaf(f, w.w, v[4 * e + 3]);
+        }
+      }
+    }
+    if (row.in) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += store_pair(A, row.token, row.head, 16 * b + 2 * e, v[2 * e], v[2 * e + 1]);
+    }
+  }
+  if (row.in && A.out_row_sum) atomicAdd(A.out_row_sum + row.token, sum);
+  return make_float2(m, z);
 }
 
 template <int kSteps>
@@ -110,6 +215,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
   using Sh = Shared<kSteps>;
   constexpr int dh = 16 * kSteps;
   constexpr int kPart = kTileRows * (dh + 2);             // floats of a tile's part
+  // blocks of 16 channels that an output row is staged by
+  constexpr int kStage = kSteps % 4 == 0 ? 4 : kSteps % 3 == 0 ? 3 : kSteps % 2 == 0 ? 2 : 1;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   Sh& S = *reinterpret_cast<Sh*>(smem_raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -121,12 +228,15 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
       mbar_init(smem_u32(&S.v_empty[i]), 1);
       mbar_init(smem_u32(&S.q_full[i]), 4);
       mbar_init(smem_u32(&S.s_full[i]), 1);
-      mbar_init(smem_u32(&S.p_full[i]), 4);
+      mbar_init(smem_u32(&S.p_full[i][0]), 4);
+      mbar_init(smem_u32(&S.p_full[i][1]), 4);
+      mbar_init(smem_u32(&S.pv_half[i]), 1);
       mbar_init(smem_u32(&S.pv_done[i]), 1);
       mbar_init(smem_u32(&S.o_empty[i]), 4);
       mbar_init(smem_u32(&S.item_full[i]), 1);
       mbar_init(smem_u32(&S.item_empty[i]), kSoftWarps + kConvWarps + 1);
     }
+    mbar_init(smem_u32(&S.ask), 1);
     mbar_init(smem_u32(&S.done), 1);
     S.abort = 0;
     if (smem_u32(smem_raw) & 1023u) {
@@ -150,25 +260,27 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
   // ---- the line of items: requests in order
   const int per = (P.a.requests + kThreads - 1) / kThreads;
   {
-    long long n = 0;
-    for (int b = tid * per; b < min((tid + 1) * per, P.a.requests); ++b) n += (long long)pairs_of(P, request_of(P.a, b)) * P.a.c.kv_heads;
-    long long before = n;
+    int n = 0;
+#pragma unroll 1
+    for (int b = tid * per; b < min((tid + 1) * per, P.a.requests); ++b) n += pairs_of(P, request_of(P.a, b)) * P.a.c.kv_heads;
+    int before = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long a = __shfl_up_sync(0xffffffffu, before, o);
+      const int a = __shfl_up_sync(0xffffffffu, before, o);
       if (lane >= o) before += a;
     }
     if (lane == 31) S.first[warp] = before;
     __syncthreads();
+#pragma unroll 1
     for (int w = 0; w < warp; ++w) before += S.first[w];
     __syncthreads();
     S.first[tid + 1] = before;
     if (tid == 0) S.first[0] = 0;
     __syncthreads();
   }
-  const long long items = S.first[kThreads];
+  const int items = S.first[kThreads];
   // parts of an item along the keys
-  const int parts = items > 0 && items * 2 <= (long long)gridDim.x ? int((long long)gridDim.x / items) : 1;
+  const int parts = items > 0 && items <= int(gridDim.x) / 2 ? int(gridDim.x) / items : 1;
 
   // What every role but the fetching warp does with an item: read it, hand the slot back.
   auto next_item = [&](int it, Item& x) {
@@ -184,36 +296,37 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
     // ---------------------------------------------------------------- items
     for (int it = 0;; ++it) {
       bool ok = it < 2 || wait_for(S.item_empty[it & 1], uint32_t((it >> 1) - 1), abort, 102, P.status);
+      // (taken when the item before it is two steps from its end, so that what is left goes to who is free)
+      ok = ok && (it == 0 || wait_for(S.ask, uint32_t(it - 1), abort, 113, P.status));
       ok = __all_sync(0xffffffffu, ok);
       if (lane == 0) {
         Item x = {};
         x.b = -1;
-        const long long ticket = ok ? atomicAdd(P.tickets, 1) : items * parts;
+        const int ticket = ok ? atomicAdd(P.tickets, 1) : items * parts;
         if (ticket < items * parts) {
-          const long long id = ticket / parts;
+          const int id = ticket / parts;
           int lo = 0, hi = kThreads - 1;
           while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (S.first[mid] <= id) lo = mid; else hi = mid - 1;
           }
-          long long start = S.first[lo];
-          int b = lo * per;
+          int start = S.first[lo], b = lo * per;
           Request rq = request_of(P.a, b);
           int pairs = pairs_of(P, rq);
-          while (id >= start + (long long)pairs * P.a.c.kv_heads) {
-            start += (long long)pairs * P.a.c.kv_heads;
+          while (id >= start + pairs * P.a.c.kv_heads) {
+            start += pairs * P.a.c.kv_heads;
             rq = request_of(P.a, ++b);
             pairs = pairs_of(P, rq);
           }
-          const int local = int(id - start), up = local / P.a.c.kv_heads;
+          const int local = id - start, up = local / P.a.c.kv_heads;
           x.b = b;
           x.h = local - up * P.a.c.kv_heads;
           x.row0 = (pairs - 1 - up) * kPair;
           x.q0 = rq.q0;
           x.before = rq.kv - rq.q_true;
           x.n_rows = rq.q_len * P.a.group;
-          x.part = int(ticket - id * parts);
-          x.id = int(id);
+          x.part = ticket - id * parts;
+          x.id = id;
           int steps[2], most = 0;
           for (int i = 0; i < 2; ++i) {
             const int rows = min(x.n_rows - x.row0 - i * kTileRows, kTileRows);
@@ -240,8 +353,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
   } else if (warp == kMmaWarp) {
     // ---------------------------------------------------------------- MMAs
     const bool issues = elect_one();
-    // D = f32, A and B f16; S: both K-major, N = 128; P V: A in tensor memory, B MN-major, N = d_h
-    constexpr uint32_t idesc_s = (1u << 4) | (uint32_t(kKeys >> 3) << 17) | (uint32_t(kTileRows >> 4) << 24);
+    // D = f32; S: A and B bf16, K-major, N = 128; P V: f16, A in tensor memory, B MN-major, N = d_h
+    constexpr uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(kKeys >> 3) << 17) | (uint32_t(kTileRows >> 4) << 24);
     constexpr uint32_t idesc_o = (1u << 4) | (1u << 16) | (uint32_t(dh >> 3) << 17) | (uint32_t(kTileRows >> 4) << 24);
     const uint64_t dq0 = smem_desc_sw128(smem_u32(S.q[0])), dk0 = smem_desc_sw128(smem_u32(S.k[0])),
                    dv0 = smem_desc_sw128(smem_u32(S.v[0]), 128 * 128);
@@ -251,6 +364,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
     Item x;
     for (int it = 0; ok && next_item(it, x); ++it) {
       const int n = max(x.end[0], x.end[1]) - x.j0;
+      if (n <= 2 && lane == 0) mbar_arrive(smem_u32(&S.ask));
       if (n <= 0) continue;
       auto issue_s = [&](int i, uint32_t slot) {
         if (issues) {
@@ -272,6 +386,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
         return ok;
       };
       if (!keys_ready()) break;
+#pragma unroll 1
       for (int i = 0; i < 2 && ok; ++i) {
         if (x.end[i] <= x.j0) continue;
         ok = __all_sync(0xffffffffu, wait_for(S.q_full[i], ph_q >> i, abort, 104, P.status));
@@ -284,26 +399,35 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
       if (issues) umma_commit(smem_u32(&S.k_empty[kg & 1]));
       __syncwarp();
       ++kg;
+#pragma unroll 1
       for (int j = 0; j < n && ok; ++j, ++vg) {
         const bool more = j + 1 < n;
+        if (j + 3 == n && lane == 0) mbar_arrive(smem_u32(&S.ask));
         bool keys = false, values = false;
+#pragma unroll 1
         for (int i = 0; i < 2; ++i) {
           if (x.j0 + j >= x.end[i]) continue;
-          ok = wait_for(S.p_full[i], ph_p >> i, abort, 105, P.status);
-          if (ok && !values) { ok = wait_for(S.v_full[vg & 1], vg >> 1, abort, 106, P.status); values = true; }
+          if (!values) { ok = wait_for(S.v_full[vg & 1], vg >> 1, abort, 106, P.status); values = true; }
           if (ok && j == 0) ok = wait_for(S.o_empty[i], (ph_o >> i) ^ 1u, abort, 107, P.status);
-          if (!(ok = __all_sync(0xffffffffu, ok))) break;
+          // (the weights come in two halves)
+#pragma unroll 1
+          for (int half = 0; half < 2 && ok; ++half) {
+            ok = wait_for(S.p_full[i][half], ph_p >> i, abort, 105, P.status);
+            if (!(ok = __all_sync(0xffffffffu, ok))) break;
+            tc_fence_after();
+            if (issues) {
+              const uint64_t b = dv0 + uint64_t((vg & 1) * (Sh::kTile >> 4)) + uint64_t(half * 64 * 128 / 16);
+#pragma unroll
+              for (int s = 0; s < kKeys / 32; ++s)
+                umma_f16_ts(tmem + 256u + uint32_t(i * 128), tmem + uint32_t(i * 128 + half * 32 + 8 * s), b + uint64_t(16 * 128 / 16 * s), idesc_o,
+                            j != 0 || half != 0 || s != 0 ? 1u : 0u);
+              umma_commit(smem_u32(half ? &S.pv_done[i] : &S.pv_half[i]));
+            }
+            __syncwarp();
+          }
+          if (!ok) break;
           ph_p ^= 1u << i;
           if (j == 0) ph_o ^= 1u << i;
-          tc_fence_after();
-          if (issues) {
-            const uint64_t b = dv0 + uint64_t((vg & 1) * (Sh::kTile >> 4));
-#pragma unroll
-            for (int s = 0; s < kKeys / 16; ++s)
-              umma_f16_ts(tmem + 256u + uint32_t(i * 128), tmem + uint32_t(i * 128 + 8 * s), b + uint64_t(16 * 128 / 16 * s), idesc_o, j != 0 || s != 0 ? 1u : 0u);
-            umma_commit(smem_u32(&S.pv_done[i]));
-          }
-          __syncwarp();
           if (x.j0 + j + 1 < x.end[i]) {
             if (!keys) { if (!keys_ready()) break; keys = true; }
             issue_s(i, kg & 1);
@@ -334,73 +458,88 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
       if (n <= 0) continue;
       const int32_t* table = A.table + x.b * A.ld_table;
       const int seen = min(min(x.before + (min(x.row0 + kPair, x.n_rows) - 1) / A.group + 1, A.max_kv), int(min((long long)A.table_width << A.shift, (long long)INT32_MAX)));
+      // This thread's pieces of 16 codes.  Heads of 128 channels: eight neighbouring lanes take four pieces of two rows, whose places
+      // in the tile lie in different banks.
+      auto row_at = [&](int i) { return kSteps == 8 ? i * 16 + ((t >> 4) << 1 | (t >> 2 & 1)) : (i * 128 + t) / kSteps; };
+      auto piece_of = [&](int i) { return kSteps == 8 ? (t & 3) | (t >> 3 & 1) << 2 : (i * 128 + t) % kSteps; };
+      // where they lie in K and V, in units of 16 bytes; kNone: no such block
+      constexpr uint32_t kNone = 0xffffffffu;
+      uint32_t place[kPer];
       int page[kPer];
+      const uint32_t block_units = uint32_t(A.c.kv_heads * kSteps) << A.shift, head_units = uint32_t(x.h * kSteps) << A.shift;
       auto pages_of = [&](int j) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-          const int key = (x.j0 + j) * kKeys + (i * 128 + t) / kSteps;
-          page[i] = key < seen ? __ldg(table + (key >> A.shift)) : -1;
+          const int key = (x.j0 + j) * kKeys + row_at(i);
+          page[i] = -1;
+          if (j < n && key < seen) asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(page[i]) : "l"(table + (key >> A.shift)));
         }
       };
-      uint4 raw[kPer];
-      auto fetch = [&](const uint8_t* codes, int j) {
+      auto places = [&]() {                               // (steps begin blocks)
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          const int e = i * 128 + t, r = e / kSteps, p = e - r * kSteps;
-          const int key = (x.j0 + j) * kKeys + r;
-          raw[i] = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
-          if (unsigned(page[i]) < unsigned(A.c.num_blocks)) {
-            const int64_t row = ((int64_t(page[i]) * A.c.kv_heads + x.h) << A.shift) + (key & ((1 << A.shift) - 1));
-            raw[i] = __ldg(reinterpret_cast<const uint4*>(codes + row * dh) + p);
-          }
-        }
+        for (int i = 0; i < kPer; ++i)
+          place[i] = unsigned(page[i]) < unsigned(A.c.num_blocks)
+                         ? uint32_t(page[i]) * block_units + head_units + uint32_t((row_at(i) & ((1 << A.shift) - 1)) * kSteps + piece_of(i))
+                         : kNone;
       };
-      auto convert = [&](uint8_t* tile) {
+      // Codes are asked for a step ahead: K and V of it are in flight while this step's are converted.  (Pieces of no block keep any bytes:
+      // their tokens weigh nothing.)
+      uint4 raw_k[kPer] = {}, raw_v[kPer] = {};
+      auto fetch = [&](uint4 (&raw)[kPer], const uint8_t* codes) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          // (volatile: the compiler would otherwise move the load down to its use)
+          if (place[i] != kNone)
+            asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "+r"(raw[i].x), "+r"(raw[i].y), "+r"(raw[i].z), "+r"(raw[i].w) : "l"(codes + uint64_t(place[i]) * 16));
+      };
+      auto convert = [&](const uint4 (&raw)[kPer], uint8_t* tile, bool k) {
+        auto lo = [&](uint32_t w) { return k ? bf16_codes(w, 0x4140) : codes_lo(w); };
+        auto hi = [&](uint32_t w) { return k ? bf16_codes(w, 0x4342) : codes_hi(w); };
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-          const int e = i * 128 + t, r = e / kSteps, p = e - r * kSteps;
-          const uint4 a = make_uint4(codes_lo(raw[i].x), codes_hi(raw[i].x), codes_lo(raw[i].y), codes_hi(raw[i].y));
-          const uint4 b = make_uint4(codes_lo(raw[i].z), codes_hi(raw[i].z), codes_lo(raw[i].w), codes_hi(raw[i].w));
-          const bool odd = (p >> 2) & 1;                  // (the second block's lanes write their halves the other way round: no bank conflicts)
-          *reinterpret_cast<uint4*>(tile + piece_at(r, 2 * p + (odd ? 1 : 0))) = odd ? b : a;
-          *reinterpret_cast<uint4*>(tile + piece_at(r, 2 * p + (odd ? 0 : 1))) = odd ? a : b;
+          const int r = row_at(i), p = piece_of(i);
+          *reinterpret_cast<uint4*>(tile + piece_at(r, 2 * p)) = make_uint4(lo(raw[i].x), hi(raw[i].x), lo(raw[i].y), hi(raw[i].y));
+          *reinterpret_cast<uint4*>(tile + piece_at(r, 2 * p + 1)) = make_uint4(lo(raw[i].z), hi(raw[i].z), lo(raw[i].w), hi(raw[i].w));
         }
         fence_async_smem();
         __syncwarp();
       };
       // the scales of eight groups of 16 keys
-      float4 sc = make_float4(1.f, -CUDART_INF_F, 0.f, 0.f);
+      float ks = 0.f, vs = 0.f;                           // (0: no block; its tokens weigh nothing)
       auto fetch_scales = [&](int j) {
         if (t < 8) {
           const int key = (x.j0 + j) * kKeys + 16 * t;
-          const int pg = key < seen ? __ldg(table + (key >> A.shift)) : -1;
-          sc = make_float4(1.f, -CUDART_INF_F, 0.f, 0.f);                    // (tokens of a missing block weigh nothing)
+          const int pg = j < n && key < seen ? __ldg(table + (key >> A.shift)) : -1;
+          vs = 0.f;
           if (unsigned(pg) < unsigned(A.c.num_blocks)) {
             const int64_t at = int64_t(pg) * A.c.kv_heads + x.h;
-            const float vs = __ldg(A.c.v_scale + at);
-            sc = make_float4(__ldg(A.c.k_scale + at), lg2(vs), __fdividef(1.f, vs), 0.f);
+            asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(ks) : "l"(A.c.k_scale + at));
+            asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(vs) : "l"(A.c.v_scale + at));
           }
         }
       };
       pages_of(0);
-      fetch(A.c.k_codes, 0);
-      fetch_scales(0);
-      for (int j = 0; j < n; ++j) {
-        if (!(ok = __all_sync(0xffffffffu, wait_for(S.k_empty[kg & 1], (kg >> 1) ^ 1u, abort, 108, P.status)))) break;
-        if (t < 8) S.scale[kg & 3][t] = sc;
-        convert(S.k[kg & 1]);
-        if (lane == 0) mbar_arrive(smem_u32(&S.k_full[kg & 1]));
-        ++kg;
-        fetch(A.c.v_codes, j);
-        if (j + 1 < n) fetch_scales(j + 1);
-        if (!(ok = __all_sync(0xffffffffu, wait_for(S.v_empty[vg & 1], (vg >> 1) ^ 1u, abort, 109, P.status)))) break;
-        convert(S.v[vg & 1]);
-        if (lane == 0) mbar_arrive(smem_u32(&S.v_full[vg & 1]));
-        ++vg;
-        if (j + 1 < n) {
-          pages_of(j + 1);
-          fetch(A.c.k_codes, j + 1);
+#pragma unroll 1
+      for (int j = -1; j < n; ++j) {
+        if (j >= 0) {
+          if (!(ok = __all_sync(0xffffffffu, wait_for(S.k_empty[kg & 1], (kg >> 1) ^ 1u, abort, 108, P.status)))) break;
+          if (t < 8) S.scale[kg & 3][t] = vs > 0.f ? make_float4(ks, lg2(vs), __fdividef(1.f, vs), 0.f) : make_float4(1.f, -CUDART_INF_F, 0.f, 0.f);
+          convert(raw_k, S.k[kg & 1], true);
+          if (lane == 0) mbar_arrive(smem_u32(&S.k_full[kg & 1]));
+          ++kg;
         }
+        places();
+        fetch(raw_k, A.c.k_codes);                        // (past the last step: no places, nothing is read)
+        fetch_scales(j + 1);
+        if (j >= 0) {
+          if (!(ok = __all_sync(0xffffffffu, wait_for(S.v_empty[vg & 1], (vg >> 1) ^ 1u, abort, 109, P.status)))) break;
+          convert(raw_v, S.v[vg & 1], false);
+          if (lane == 0) mbar_arrive(smem_u32(&S.v_full[vg & 1]));
+          ++vg;
+        }
+        fetch(raw_v, A.c.v_codes);
+        pages_of(j + 2);
       }
     }
   } else if (warp < kSoftWarps) {
@@ -415,155 +554,152 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
       if (i == 0) asm volatile("bar.sync 1, 128;" ::: "memory");
       else asm volatile("bar.sync 2, 128;" ::: "memory");
     };
+    // An item stays in shared memory until its output is written; what the step loop needs of it is in registers.
+    auto see_item = [&](int it) {
+      bool there = wait_for(S.item_full[it & 1], uint32_t(it >> 1), abort, 101, P.status);
+      there = __all_sync(0xffffffffu, there);
+      return there && S.item[it & 1].b >= 0;
+    };
+    // a thread's row of an item
+    auto row_of = [&](const volatile Item& x) {
+      const int row = x.row0 + i * kTileRows + r, t = row / A.group;
+      return OutRow{x.q0 + t, x.h * A.group + row - t * A.group, row < x.n_rows};
+    };
+    // the warp's 32 query rows into the swizzled tile, asynchronously; rows past the item's are zeros
+    auto ask_q = [&](const volatile Item& x) {
+      const OutRow row = row_of(x);
+      const long long off = row.in ? row.token * A.q_st + row.head * A.q_sh : -1;
+      constexpr int kPieces = 2 * kSteps;                 // 16-byte pieces of a row
+#pragma unroll 4
+      for (int e = lane; e < 32 * kPieces; e += 32) {
+        const int rr = e / kPieces, c = e - rr * kPieces;
+        const long long at = __shfl_sync(0xffffffffu, off, rr);
+        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(A.q) + (at < 0 ? 0 : at) + 8 * c;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                     ::"r"(smem_u32(S.q[i] + piece_at(quarter * 32 + rr, c))), "l"(src), "r"(at < 0 ? 0 : 16) : "memory");
+      }
+    };
+    auto give_q = [&]() {
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&S.q_full[i]));
+    };
     bool ok = true;
-    Item x;
-    for (int it = 0; ok && next_item(it, x); ++it) {
-      const int n_both = max(max(x.end[0], x.end[1]) - x.j0, 0), n = x.end[i] - x.j0;
-      const int row = x.row0 + i * kTileRows + r;
-      const bool in = row < x.n_rows;
-      const int row_token = row / A.group, token = x.q0 + row_token, head = x.h * A.group + row - row_token * A.group;
-      const int limit = in ? min(x.before + row_token + 1, A.max_kv) : 0;
-      float m = -CUDART_INF_F, z = 0.f;
-      if (n > 0) {
-        // ---- queries to f16, the row's largest element in [2^8, 2^9)
-        float back;
-        {
-          const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(A.q) + token * A.q_st + head * A.q_sh;
-          float top = 0.f;
-#pragma unroll 4
-          for (int c = 0; c < 2 * kSteps; ++c) {
-            const uint4 w = in ? __ldg(reinterpret_cast<const uint4*>(p) + c) : make_uint4(0u, 0u, 0u, 0u);
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              top = max3(top, __uint_as_float((u[e] << 16) & 0x7fffffffu), __uint_as_float(u[e] & 0x7fff0000u));
-          }
-          const int e2 = min(max(int(__float_as_uint(top) >> 23) - 127 - 8, -110), 110);
-          const float down = __uint_as_float(uint32_t(127 - e2) << 23);
-          back = __uint_as_float(uint32_t(127 + e2) << 23) * A.scale;
-#pragma unroll 4
-          for (int c = 0; c < 2 * kSteps; ++c) {          // (read again, from L1)
-            const uint4 w = in ? __ldg(reinterpret_cast<const uint4*>(p) + c) : make_uint4(0u, 0u, 0u, 0u);
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-            uint32_t h[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              h[e] = bits_of(__floats2half2_rn(__uint_as_float(u[e] << 16) * down, __uint_as_float(u[e] & 0xffff0000u) * down));
-            *reinterpret_cast<uint4*>(S.q[i] + piece_at(r, c)) = make_uint4(h[0], h[1], h[2], h[3]);
-          }
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&S.q_full[i]));
-        }
-        for (int j = 0; j < n; ++j) {
-          if (!(ok = __all_sync(0xffffffffu, wait_for(S.s_full[i], ph_s, abort, 110, P.status)))) break;
-          ph_s ^= 1u;
-          tc_fence_after();
-          const int sees = limit - (x.j0 + j) * kKeys;    // columns of this step
-          const bool masked = __any_sync(0xffffffffu, sees < kKeys);
-          const float4* scale = S.scale[(kg + j) & 3];
-          uint32_t buf[2][16];
-          tmem_ld16(t_s, buf[0]);
-#pragma unroll
-          for (int c = 0; c < kKeys / 16; ++c) {          // 16 keys: a block of tokens, or a part of one
-            uint32_t (&s)[16] = buf[c & 1];
-            tmem_ld_wait(s);
-            if (c + 1 < kKeys / 16) tmem_ld16(t_s + 16u * (c + 1), buf[(c + 1) & 1]);
+    bool more = see_item(0);
+    if (more && S.item[0].end[i] > S.item[0].j0) { ask_q(S.item[0]); give_q(); }
+    for (int it = 0; more; ++it) {
+      const volatile Item& x = S.item[it & 1];
+      const int n = x.end[i] - x.j0;
+      int sees = 0;                                       // keys that the row sees, from the item's first on
+      {
+        const OutRow row = row_of(x);
+        if (row.in) sees = min(x.before + row.token - x.q0 + 1, A.max_kv) - x.j0 * kKeys;
+      }
+      float m = -CUDART_INF_F, z = 0.f, base = 0.f;       // base: kLift - m, 0 where nothing has been seen
+      for (int j = 0; j < n; ++j) {
+        if (!(ok = __all_sync(0xffffffffu, wait_for(S.s_full[i], ph_s, abort, 110, P.status)))) break;
+        ph_s ^= 1u;
+        tc_fence_after();
+        const bool masked = __any_sync(0xffffffffu, sees < kKeys);
+        const float4* scale = S.scale[(kg + j) & 3];
+        // 32 keys: exponents on the m so far, and the columns' maximum beside them; if it turns out too far above m, m moves and
+        // the columns are read again
+        auto group = [&](uint32_t (&s)[32], int c) {
+          const float4 g0 = scale[2 * c], g1 = scale[2 * c + 1];
+          const float f0 = g0.x * A.scale, f1 = g1.x * A.scale;
+#pragma unroll 1
+          for (;;) {
+            tmem_ld_wait32(s);
             if (masked) {
 #pragma unroll
-              for (int e = 0; e < 16; ++e)
-                if (16 * c + e >= sees) s[e] = 0xff800000u;
+              for (int e = 0; e < 32; ++e)
+                if (32 * c + e >= sees) s[e] = 0xff800000u;
             }
-            const float4 g = scale[c];
-            const float f = g.x * back;
-            float top = __uint_as_float(s[0]);
+            float t0 = __uint_as_float(s[0]), t1 = __uint_as_float(s[16]);
 #pragma unroll
-            for (int e = 1; e < 15; e += 2) top = max3(top, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-            top = fmaf(fmaxf(top, __uint_as_float(s[15])), f, g.y);
-            if (__any_sync(0xffffffffu, top > m + kLag)) {
-              // m rises: what has been summed and written so far is brought down
-              if (c + 1 < kKeys / 16) tmem_ld_wait(buf[(c + 1) & 1]);   // (no registers in flight past this point)
-              const float up = top > m + kLag ? top : m;
-              const float down = m == -CUDART_INF_F ? 0.f : ex2(m - up);
-              z *= down;
-              m = up;
-              const __half2 dh2 = __float2half2_rn(down);
-#pragma unroll 1
-              for (int b = 0; b < (c + 1) / 2; ++b) {     // (an odd last group's eight columns with what follows them)
-                uint32_t w[16];
-                tmem_ld16(t_s + 16u * b, w);
-                tmem_ld_wait(w);
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                  if (16 * b + e < 8 * c) w[e] = bits_of(__hmul2(half2_of(w[e]), dh2));
-                tmem_st16(t_s + 16u * b, w);
-              }
-              if (j > 0) {
-                // (the phase of the step before: nothing else waits for it in between)
-                if (!(ok = __all_sync(0xffffffffu, wait_for(S.pv_done[i], ph_pv ^ 1u, abort, 111, P.status)))) break;
-                tc_fence_after();
-#pragma unroll 1
-                for (int b = 0; b < kSteps; ++b) {
-                  uint32_t w[16];
-                  tmem_ld16(t_o + 16u * b, w);
-                  tmem_ld_wait(w);
-#pragma unroll
-                  for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * down);
-                  tmem_st16(t_o + 16u * b, w);
-                }
-              }
-              tmem_st_wait();
+            for (int e = 1; e < 15; e += 2) {
+              t0 = max3(t0, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+              t1 = max3(t1, __uint_as_float(s[16 + e]), __uint_as_float(s[17 + e]));
             }
-            const float base = m == -CUDART_INF_F ? 0.f : kLift - m;
-            const f32x2 ff = splat2(f), bb = splat2(base + g.y);
-            f32x2 sum = splat2(0.f);
-            uint32_t w[8];
+            const float top = fmaxf(fmaf(fmaxf(t0, __uint_as_float(s[15])), f0, g0.y), fmaf(fmaxf(t1, __uint_as_float(s[31])), f1, g1.y));
+            const f32x2 ff0 = splat2(f0), ff1 = splat2(f1), b0 = splat2(base + g0.y), b1 = splat2(base + g1.y);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 16; ++e) {
               float a, b;
-              unpack2(fma2(pack2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), ff, bb), a, b);
-              a = ex2(a);
-              b = ex2(b);
-              sum = add2(sum, pack2(a, b));
-              w[e] = bits_of(__floats2half2_rn(a, b));
+              unpack2(fma2(pack2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), e < 8 ? ff0 : ff1, e < 8 ? b0 : b1), a, b);
+              s[2 * e] = __float_as_uint(ex2(a));
+              s[2 * e + 1] = __float_as_uint(ex2(b));
             }
-            float a, b;
-            unpack2(sum, a, b);
-            z = fmaf(a + b, g.z, z);
-            tmem_st8(t_s + 8u * c, w);
+            if (!__any_sync(0xffffffffu, top > m + kLag)) break;
+            // m rises: what has been summed and written so far is brought down
+            const float up = top > m + kLag ? top : m;
+            const float down = m == -CUDART_INF_F ? 0.f : ex2(m - up);
+            z *= down;
+            m = up;
+            base = m == -CUDART_INF_F ? 0.f : kLift - m;
+            if (j > 0 || c >= 2) {
+              // the accumulator, once it has the weights handed over so far: the step before's, or this step's first half
+              ok = c < 2 ? wait_for(S.pv_done[i], ph_pv ^ 1u, abort, 111, P.status) : wait_for(S.pv_half[i], ph_pv, abort, 114, P.status);
+              if (!(ok = __all_sync(0xffffffffu, ok))) break;
+              tc_fence_after();
+            }
+            bring_down(t_s, c & ~1, c, t_o, j > 0 || c >= 2 ? kSteps : 0, down);     // (weights that have not been handed over)
+            tmem_ld32(t_s + 32u * c, s);
           }
+          f32x2 sum0 = splat2(0.f), sum1 = splat2(0.f);
+          uint32_t w[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float a = __uint_as_float(s[2 * e]), b = __uint_as_float(s[2 * e + 1]);
+            if (e < 8) sum0 = add2(sum0, pack2(a, b)); else sum1 = add2(sum1, pack2(a, b));
+            w[e] = bits_of(__floats2half2_rn(a, b));
+          }
+          if (c < 3) tmem_ld32(t_s + 32u * (c + 1), s);
+          tmem_st16(t_s + 16u * c, w);
+          float a, b;
+          unpack2(sum0, a, b);
+          z = fmaf(a + b, g0.z, z);
+          unpack2(sum1, a, b);
+          z = fmaf(a + b, g1.z, z);
+        };
+        uint32_t s[32];
+        tmem_ld32(t_s, s);
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          group(s, c);
           if (!ok) break;
-          tmem_st_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&S.p_full[i]));
-          ph_pv ^= 1u;                                    // this step's completion comes next
+          if (c & 1) {
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&S.p_full[i][c >> 1]));
+          }
         }
         if (!ok) break;
+        sees -= kKeys;
+        ph_pv ^= 1u;                                      // this step's completion comes next
+      }
+      if (!ok) break;
+      // the next item's queries come while the last product and the output run (the S MMAs have read this one's)
+      more = see_item(it + 1);
+      const volatile Item& y = S.item[(it + 1) & 1];
+      const bool q_next = more && y.end[i] > y.j0;
+      if (q_next) ask_q(y);
+      if (n > 0) {
         ok = __all_sync(0xffffffffu, wait_for(S.pv_done[i], ph_pv ^ 1u, abort, 112, P.status));
-        if (!ok) break;
         tc_fence_after();
       }
-      kg += uint32_t(n_both);
+      if (q_next) give_q();
+      if (!ok) break;
+      kg += uint32_t(max(max(x.end[0], x.end[1]) - x.j0, 0));
+      const OutRow row = row_of(x);
 
       // ---- the row
-      const bool whole = parts == 1;
-      float* part = A.partials + (int64_t(x.id) * parts * 2 + x.part * 2 + i) * kPart;
-      bool writes = whole;
-      if (!whole) {
-        if (n > 0) {
-#pragma unroll
-          for (int b = 0; b < kSteps; ++b) {
-            uint32_t w[16];
-            tmem_ld16(t_o + 16u * b, w);
-            tmem_ld_wait(w);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              __stcg(reinterpret_cast<uint4*>(part) + (4 * b + e) * kTileRows + r, make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]));
-          }
-        }
-        __stcg(reinterpret_cast<float2*>(part + kTileRows * dh) + r, make_float2(n > 0 ? m : -CUDART_INF_F, n > 0 ? z : 0.f));
-        __threadfence();
+      bool writes = true;
+      const float* parts0 = A.partials + (int64_t(x.id) * parts * 2 + i) * kPart;
+      if (parts > 1) {
+        put_part<kSteps>(const_cast<float*>(parts0) + int64_t(2 * x.part) * kPart, r, t_o, n > 0, m, z);
         tile_barrier();
         if (r == 0) {
           const int seen = atomicAdd(A.counters + 2 * x.id + i, 1);
@@ -575,52 +711,44 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
         if (writes) __threadfence();
       }
       if (writes) {
-        const float* p0 = A.partials + (int64_t(x.id) * parts * 2 + i) * kPart;
-        float zt = z, mt = m;
-        if (!whole) {
-          mt = -CUDART_INF_F;
-          for (int p = 0; p < parts; ++p) mt = fmaxf(mt, __ldcg(reinterpret_cast<const float2*>(p0 + int64_t(2 * p) * kPart + kTileRows * dh) + r).x);
-          zt = 0.f;
-          for (int p = 0; p < parts; ++p) {
-            const float2 mz = __ldcg(reinterpret_cast<const float2*>(p0 + int64_t(2 * p) * kPart + kTileRows * dh) + r);
-            if (mz.x > -CUDART_INF_F) zt = fmaf(ex2(mz.x - mt), mz.y, zt);
-          }
-        }
-        const float inv = zt > 0.f ? __fdividef(1.f, zt) : zt == 0.f ? 0.f : CUDART_NAN_F;
-        int sum = 0;
-#pragma unroll
-        for (int b = 0; b < kSteps; ++b) {
-          float v[16];
-          if (whole) {
-            uint32_t w[16] = {};
-            if (n > 0) {
-              tmem_ld16(t_o + 16u * b, w);
-              tmem_ld_wait(w);
-            }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(w[e]) * inv;
-          } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = 0.f;
-            for (int p = 0; p < parts; ++p) {
-              const float* pp = p0 + int64_t(2 * p) * kPart;
-              const float mp = __ldcg(reinterpret_cast<const float2*>(pp + kTileRows * dh) + r).x;
-              if (mp == -CUDART_INF_F) continue;          // (saw nothing, wrote nothing)
-              const float f = ex2(mp - mt) * inv;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float4 w = __ldcg(reinterpret_cast<const float4*>(pp) + (4 * b + e) * kTileRows + r);
-                v[4 * e] = fmaf(f, w.x, v[4 * e]);
-                v[4 * e + 1] = fmaf(f, w.y, v[4 * e + 1]);
-                v[4 * e + 2] = fmaf(f, w.z, v[4 * e + 2]);
-                v[4 * e + 3] = fmaf(f, w.w, v[4 * e + 3]);
+        float2 mz = make_float2(m, z);
+        if (A.out_kind == REPQ_OUT_BF16 && parts == 1) {
+          // 64 channels at a time through shared memory: a store of the warp then covers whole rows, not 16 bytes of 32
+          const float inv = z > 0.f ? __fdividef(1.f, z) : z == 0.f ? 0.f : CUDART_NAN_F;
+          uint8_t* stage = S.stage[warp];
+          const long long off = row.in ? row.token * A.ldo + row.head * A.o_sh : -1;
+#pragma unroll 1
+          for (int b0 = 0; b0 < kSteps; b0 += kStage) {
+#pragma unroll 1
+            for (int b = 0; b < kStage; ++b) {
+              uint32_t w[16] = {};
+              if (n > 0) {
+                tmem_ld16(t_o + 16u * (b0 + b), w);
+                tmem_ld_wait(w);
               }
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(w[2 * e]) * inv, __uint_as_float(w[2 * e + 1]) * inv);
+                w[e] = *reinterpret_cast<const uint32_t*>(&h);
+              }
+              *reinterpret_cast<uint4*>(stage + lane * 128 + (((2 * b) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+              *reinterpret_cast<uint4*>(stage + lane * 128 + (((2 * b + 1) ^ (lane & 7)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
             }
+            __syncwarp();
+#pragma unroll 2
+            for (int e = lane; e < 32 * 2 * kStage; e += 32) {
+              const int rr = e / (2 * kStage), c = e - rr * (2 * kStage);
+              const long long at = __shfl_sync(0xffffffffu, off, rr);
+              const uint4 w = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((c ^ (rr & 7)) << 4));
+              if (at >= 0) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(A.out) + at + 16 * b0 + 8 * c) = w;
+            }
+            __syncwarp();
           }
-          if (in) sum += store16(A, token, head, 16 * b, v);
+        } else {
+          mz = put_row<kSteps>(A, row, r, t_o, n > 0, m, z, parts0, parts);
         }
-        if (in && A.out_row_sum) atomicAdd(A.out_row_sum + token, sum);
-        if (in && A.lse) A.lse[int64_t(token) * A.heads + head] = zt > 0.f ? (mt - kLift + log2f(zt)) * kLn2 : zt == 0.f ? -CUDART_INF_F : CUDART_NAN_F;
+        if (row.in && A.lse)
+          A.lse[int64_t(row.token) * A.heads + row.head] = mz.y > 0.f ? (mz.x - kLift + log2f(mz.y)) * kLn2 : mz.y == 0.f ? -CUDART_INF_F : CUDART_NAN_F;
       }
       if (n > 0) {
         tc_fence_before();
@@ -628,7 +756,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
         if (lane == 0) mbar_arrive(smem_u32(&S.o_empty[i]));
       }
       __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&S.item_empty[it & 1]));
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
   }
 
   // ------------------------------------------------------------------ teardown
