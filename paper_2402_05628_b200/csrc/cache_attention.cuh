@@ -23,6 +23,7 @@ struct AttendParams {
   int out_kind, qmax, pack4;
   float inv_so; int zo;
   void* out; int64_t ldo, o_sh;
+  int out_wide;                          // output rows are 32-byte aligned
   int32_t* out_row_sum;
   float* lse;
   int32_t* counters;                     // workspace: one per worker, zero between calls

@@ -30,7 +30,9 @@ using namespace tc;
 constexpr int kTileRows = 128, kPair = 2 * kTileRows, kKeys = 128;
 constexpr int kSoftWarps = 8, kConvWarps = 4;
 constexpr int kMmaWarp = kSoftWarps + kConvWarps, kItemWarp = kMmaWarp + 1;
-constexpr int kThreads = 32 * (kItemWarp + 1);
+constexpr int kThreads = 512;             // (two warps of the last group have nothing to do)
+// Registers per thread, dealt out anew once the roles part: 256 x 176 + 128 x 80 + 128 x 80 = the 512 x 128 of the launch
+constexpr int kSoftRegs = 176, kConvRegs = 80, kOtherRegs = 80;
 constexpr float kLift = 7.f, kLag = 8.f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -50,11 +52,10 @@ struct Shared {
   alignas(1024) uint8_t q[2][kTile];
   alignas(1024) uint8_t k[2][kTile];
   alignas(1024) uint8_t v[2][kTile];
-  alignas(16) uint8_t stage[kSoftWarps][32 * 128];                       // output rows on their way: 128 bytes of a warp's 32 rows
+  alignas(16) uint8_t raw[2][128 * 16 * kSteps];                         // codes of a step's K and V on their way
   float4 scale[4][8];                    // per step (four in turn) and 16 keys: k_scale, log2 v_scale, 1 / v_scale
   Item item[2];
-  int first[kThreads + 1];               // items before a thread's requests
-  int last[2];
+  int items, last[2];
   alignas(8) uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], p_full[2][2], pv_half[2], pv_done[2], o_empty[2], item_full[2],
       item_empty[2], ask, done;
   uint32_t tmem_base;
@@ -113,18 +114,11 @@ __device__ __forceinline__ uint32_t piece_at(int r, int c) {
   return uint32_t(c >> 3) * (128u * 128u) + uint32_t(r) * 128u + (uint32_t((c ^ r) & 7) << 4);
 }
 
-// Weights of blocks [b0, b1) of 32 keys and `o_blocks` blocks of 16 accumulator columns of the warp's rows, times f.
-static __device__ __noinline__ void bring_down(uint32_t t_w, int b0, int b1, uint32_t t_o, int o_blocks, float f) {
-  const __half2 f2 = __float2half2_rn(f);
-#pragma unroll 1
-  for (int b = b0; b < b1; ++b) {
-    uint32_t w[16];
-    tmem_ld16(t_w + 16u * b, w);
-    tmem_ld_wait(w);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) w[e] = bits_of(__hmul2(half2_of(w[e]), f2));
-    tmem_st16(t_w + 16u * b, w);
-  }
+// A row's maximum rises (f = 2^(m - m'), 1 in rows that stay): `o_blocks` blocks of 16 accumulator columns of the warp's rows times f, once
+// the accumulator has the weights handed over so far.
+static __device__ __noinline__ bool bring_down(uint64_t& bar, uint32_t parity, volatile int* abort, int32_t* status, uint32_t t_o, int o_blocks, float f) {
+  if (!__all_sync(0xffffffffu, wait_for(bar, parity, abort, 111, status))) return false;
+  tc_fence_after();
 #pragma unroll 1
   for (int b = 0; b < o_blocks; ++b) {
     uint32_t w[16];
@@ -135,6 +129,7 @@ static __device__ __noinline__ void bring_down(uint32_t t_w, int b0, int b1, uin
     tmem_st16(t_o + 16u * b, w);
   }
   tmem_st_wait();
+  return true;
 }
 
 // A tile's part of an item that is cut along the keys: accumulators, m and Z of its rows (a row per thread).
@@ -155,7 +150,7 @@ __device__ __noinline__ void put_part(float* part, int r, uint32_t t_o, bool any
   __threadfence();
 }
 
-// The output of a row that does not leave by whole bf16 rows: parts joined in order, or (one part) the accumulators; any kind of output.
+// The output of a row: the accumulators, or parts joined in order.
 struct OutRow { int token, head; bool in; };
 template <int kSteps>
 __device__ __noinline__ float2 put_row(const AttendParams& A, OutRow row, int r, uint32_t t_o, bool any, float m, float z, const float* parts0, int parts) {
@@ -201,8 +196,23 @@ __device__ __noinline__ float2 put_row(const AttendParams& A, OutRow row, int r,
         }
       }
     }
-    if (row.in) {
+    if (row.in && A.out_kind == REPQ_OUT_BF16) {
+      uint32_t w[8];
 #pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+        w[e] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+      __nv_bfloat16* o = static_cast<__nv_bfloat16*>(A.out) + row.token * A.ldo + row.head * A.o_sh + 16 * b;
+      if (A.out_wide) {                                   // (half the passes of a store that touches 32 rows)
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     ::"l"(o), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+      } else {
+        reinterpret_cast<uint4*>(o)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(o)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+      }
+    } else if (row.in) {
+#pragma unroll 1
       for (int e = 0; e < 8; ++e) sum += store_pair(A, row.token, row.head, 16 * b + 2 * e, v[2 * e], v[2 * e + 1]);
     }
   }
@@ -215,8 +225,6 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
   using Sh = Shared<kSteps>;
   constexpr int dh = 16 * kSteps;
   constexpr int kPart = kTileRows * (dh + 2);             // floats of a tile's part
-  // blocks of 16 channels that an output row is staged by
-  constexpr int kStage = kSteps % 4 == 0 ? 4 : kSteps % 3 == 0 ? 3 : kSteps % 2 == 0 ? 2 : 1;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   Sh& S = *reinterpret_cast<Sh*>(smem_raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -257,28 +265,17 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
   grid_dependency_wait();
   grid_dependency_trigger();
 
-  // ---- the line of items: requests in order
-  const int per = (P.a.requests + kThreads - 1) / kThreads;
+  // ---- items: row pairs of all requests, times heads
+  if (tid == 0) S.items = 0;
+  __syncthreads();
   {
     int n = 0;
 #pragma unroll 1
-    for (int b = tid * per; b < min((tid + 1) * per, P.a.requests); ++b) n += pairs_of(P, request_of(P.a, b)) * P.a.c.kv_heads;
-    int before = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int a = __shfl_up_sync(0xffffffffu, before, o);
-      if (lane >= o) before += a;
-    }
-    if (lane == 31) S.first[warp] = before;
-    __syncthreads();
-#pragma unroll 1
-    for (int w = 0; w < warp; ++w) before += S.first[w];
-    __syncthreads();
-    S.first[tid + 1] = before;
-    if (tid == 0) S.first[0] = 0;
-    __syncthreads();
+    for (int b = tid; b < P.a.requests; b += kThreads) n += pairs_of(P, request_of(P.a, b)) * P.a.c.kv_heads;
+    if (n > 0) atomicAdd(&S.items, n);
   }
-  const int items = S.first[kThreads];
+  __syncthreads();
+  const int items = S.items;
   // parts of an item along the keys
   const int parts = items > 0 && items <= int(gridDim.x) / 2 ? int(gridDim.x) / items : 1;
 
@@ -292,42 +289,50 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
     return x.b >= 0;
   };
 
-  if (warp == kItemWarp) {
-    // ---------------------------------------------------------------- items
-    for (int it = 0;; ++it) {
-      bool ok = it < 2 || wait_for(S.item_empty[it & 1], uint32_t((it >> 1) - 1), abort, 102, P.status);
-      // (taken when the item before it is two steps from its end, so that what is left goes to who is free)
-      ok = ok && (it == 0 || wait_for(S.ask, uint32_t(it - 1), abort, 113, P.status));
-      ok = __all_sync(0xffffffffu, ok);
-      if (lane == 0) {
+  if (warp >= kMmaWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp == kItemWarp) {
+      // ---------------------------------------------------------------- items
+      // Level k holds the k-th row pair from the end of every request that has one, for every key / value head: the longest items come
+      // first.  The warp walks the levels along with its tickets.
+      auto pairs_in = [&](int b) { return b < P.a.requests ? pairs_of(P, request_of(P.a, b)) : 0; };
+      int level = -1, level_end = 0, level_start = 0;       // items up to the level's end, and before it
+      for (int it = 0;; ++it) {
+        bool ok = it < 2 || wait_for(S.item_empty[it & 1], uint32_t((it >> 1) - 1), abort, 102, P.status);
+        // (taken when the item before it is two steps from its end, so that what is left goes to who is free)
+        ok = ok && (it == 0 || wait_for(S.ask, uint32_t(it - 1), abort, 113, P.status));
+        ok = __all_sync(0xffffffffu, ok);
+        int ticket = items * parts;
+        if (ok && lane == 0) ticket = atomicAdd(P.tickets, 1);
+        ticket = __shfl_sync(0xffffffffu, ticket, 0);
         Item x = {};
         x.b = -1;
-        const int ticket = ok ? atomicAdd(P.tickets, 1) : items * parts;
         if (ticket < items * parts) {
-          const int id = ticket / parts;
-          int lo = 0, hi = kThreads - 1;
-          while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (S.first[mid] <= id) lo = mid; else hi = mid - 1;
+          x.id = ticket / parts;
+          x.part = ticket - x.id * parts;
+          while (x.id >= level_end) {
+            ++level;
+            level_start = level_end;
+            for (int b = lane; b < P.a.requests + lane; b += 32)               // (all lanes the same number of times)
+              level_end += __popc(__ballot_sync(0xffffffffu, pairs_in(b) > level)) * P.a.c.kv_heads;
           }
-          int start = S.first[lo], b = lo * per;
-          Request rq = request_of(P.a, b);
-          int pairs = pairs_of(P, rq);
-          while (id >= start + pairs * P.a.c.kv_heads) {
-            start += pairs * P.a.c.kv_heads;
-            rq = request_of(P.a, ++b);
-            pairs = pairs_of(P, rq);
+          int nth = (x.id - level_start) / P.a.c.kv_heads, b0 = 0;
+          x.h = x.id - level_start - nth * P.a.c.kv_heads;
+          uint32_t have = __ballot_sync(0xffffffffu, pairs_in(lane) > level);
+          while (nth >= __popc(have)) {
+            nth -= __popc(have);
+            b0 += 32;
+            have = __ballot_sync(0xffffffffu, pairs_in(b0 + lane) > level);
           }
-          const int local = id - start, up = local / P.a.c.kv_heads;
-          x.b = b;
-          x.h = local - up * P.a.c.kv_heads;
-          x.row0 = (pairs - 1 - up) * kPair;
+          for (; nth > 0; --nth) have &= have - 1;
+          x.b = b0 + __ffs(have) - 1;
+          const Request rq = request_of(P.a, x.b);
+          x.row0 = (pairs_of(P, rq) - 1 - level) * kPair;
           x.q0 = rq.q0;
           x.before = rq.kv - rq.q_true;
           x.n_rows = rq.q_len * P.a.group;
-          x.part = ticket - id * parts;
-          x.id = id;
           int steps[2], most = 0;
+#pragma unroll
           for (int i = 0; i < 2; ++i) {
             const int rows = min(x.n_rows - x.row0 - i * kTileRows, kTileRows);
             const int seen = rows > 0 ? min(min(x.before + (x.row0 + i * kTileRows + rows - 1) / P.a.group + 1, rq.kv), P.a.max_kv) : 0;
@@ -336,119 +341,121 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
           }
           x.j0 = int((long long)most * x.part / parts);
           const int j1 = int((long long)most * (x.part + 1) / parts);
+#pragma unroll
           for (int i = 0; i < 2; ++i) x.end[i] = max(min(steps[i], j1), x.j0);
         }
-        S.item[it & 1] = x;
-        ok = x.b >= 0;
-      }
-      ok = __shfl_sync(0xffffffffu, ok, 0);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&S.item_full[it & 1]));
-      if (!ok) break;
-    }
-    if (lane == 0 && atomicAdd(P.tickets + 1, 1) == int(gridDim.x) - 1) {     // the counters for the next call
-      P.tickets[0] = 0;
-      P.tickets[1] = 0;
-    }
-  } else if (warp == kMmaWarp) {
-    // ---------------------------------------------------------------- MMAs
-    const bool issues = elect_one();
-    // D = f32; S: A and B bf16, K-major, N = 128; P V: f16, A in tensor memory, B MN-major, N = d_h
-    constexpr uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(kKeys >> 3) << 17) | (uint32_t(kTileRows >> 4) << 24);
-    constexpr uint32_t idesc_o = (1u << 4) | (1u << 16) | (uint32_t(dh >> 3) << 17) | (uint32_t(kTileRows >> 4) << 24);
-    const uint64_t dq0 = smem_desc_sw128(smem_u32(S.q[0])), dk0 = smem_desc_sw128(smem_u32(S.k[0])),
-                   dv0 = smem_desc_sw128(smem_u32(S.v[0]), 128 * 128);
-    uint32_t kg = 0, vg = 0;                              // steps of K and V taken
-    uint32_t ph_q = 0, ph_p = 0, ph_o = 0;                // a bit per tile
-    bool ok = true;
-    Item x;
-    for (int it = 0; ok && next_item(it, x); ++it) {
-      const int n = max(x.end[0], x.end[1]) - x.j0;
-      if (n <= 2 && lane == 0) mbar_arrive(smem_u32(&S.ask));
-      if (n <= 0) continue;
-      auto issue_s = [&](int i, uint32_t slot) {
-        if (issues) {
-          const uint64_t a = dq0 + uint64_t(i * (Sh::kTile >> 4)), b = dk0 + uint64_t(slot * (Sh::kTile >> 4));
-#pragma unroll
-          for (int s = 0; s < kSteps; ++s) {
-            const uint32_t off = uint32_t(s >> 2) * (128 * 128 / 16) + uint32_t(s & 3) * 2;
-            umma_f16(tmem + uint32_t(i * 128), a + off, b + off, idesc_s, s != 0 ? 1u : 0u);
-          }
-          umma_commit(smem_u32(&S.s_full[i]));
+        if (lane == 0) {
+          S.item[it & 1] = x;
+          mbar_arrive(smem_u32(&S.item_full[it & 1]));
         }
         __syncwarp();
-      };
-      // a step's keys: both tiles' S
-      auto keys_ready = [&]() {
-        ok = ok && wait_for(S.k_full[kg & 1], kg >> 1, abort, 103, P.status);
-        ok = __all_sync(0xffffffffu, ok);
-        tc_fence_after();
-        return ok;
-      };
-      if (!keys_ready()) break;
-#pragma unroll 1
-      for (int i = 0; i < 2 && ok; ++i) {
-        if (x.end[i] <= x.j0) continue;
-        ok = __all_sync(0xffffffffu, wait_for(S.q_full[i], ph_q >> i, abort, 104, P.status));
-        if (!ok) break;
-        ph_q ^= 1u << i;
-        tc_fence_after();
-        issue_s(i, kg & 1);
+        if (x.b < 0) break;
       }
-      if (!ok) break;
-      if (issues) umma_commit(smem_u32(&S.k_empty[kg & 1]));
-      __syncwarp();
-      ++kg;
+      if (lane == 0 && atomicAdd(P.tickets + 1, 1) == int(gridDim.x) - 1) {     // the counters for the next call
+        P.tickets[0] = 0;
+        P.tickets[1] = 0;
+      }
+    } else if (warp == kMmaWarp) {
+      // ---------------------------------------------------------------- MMAs
+      const bool issues = elect_one();
+      // D = f32; S: A and B bf16, K-major, N = 128; P V: f16, A in tensor memory, B MN-major, N = d_h
+      constexpr uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(kKeys >> 3) << 17) | (uint32_t(kTileRows >> 4) << 24);
+      constexpr uint32_t idesc_o = (1u << 4) | (1u << 16) | (uint32_t(dh >> 3) << 17) | (uint32_t(kTileRows >> 4) << 24);
+      const uint64_t dq0 = smem_desc_sw128(smem_u32(S.q[0])), dk0 = smem_desc_sw128(smem_u32(S.k[0])),
+                     dv0 = smem_desc_sw128(smem_u32(S.v[0]), 128 * 128);
+      uint32_t kg = 0, vg = 0;                              // steps of K and V taken
+      uint32_t ph_q = 0, ph_p = 0, ph_o = 0;                // a bit per tile
+      bool ok = true;
+      Item x;
+      for (int it = 0; ok && next_item(it, x); ++it) {
+        const int n = max(x.end[0], x.end[1]) - x.j0;
+        if (n <= 2 && lane == 0) mbar_arrive(smem_u32(&S.ask));
+        if (n <= 0) continue;
+        auto issue_s = [&](int i, uint32_t slot) {
+          if (issues) {
+            const uint64_t a = dq0 + uint64_t(i * (Sh::kTile >> 4)), b = dk0 + uint64_t(slot * (Sh::kTile >> 4));
 #pragma unroll 1
-      for (int j = 0; j < n && ok; ++j, ++vg) {
-        const bool more = j + 1 < n;
-        if (j + 3 == n && lane == 0) mbar_arrive(smem_u32(&S.ask));
-        bool keys = false, values = false;
-#pragma unroll 1
-        for (int i = 0; i < 2; ++i) {
-          if (x.j0 + j >= x.end[i]) continue;
-          if (!values) { ok = wait_for(S.v_full[vg & 1], vg >> 1, abort, 106, P.status); values = true; }
-          if (ok && j == 0) ok = wait_for(S.o_empty[i], (ph_o >> i) ^ 1u, abort, 107, P.status);
-          // (the weights come in two halves)
-#pragma unroll 1
-          for (int half = 0; half < 2 && ok; ++half) {
-            ok = wait_for(S.p_full[i][half], ph_p >> i, abort, 105, P.status);
-            if (!(ok = __all_sync(0xffffffffu, ok))) break;
-            tc_fence_after();
-            if (issues) {
-              const uint64_t b = dv0 + uint64_t((vg & 1) * (Sh::kTile >> 4)) + uint64_t(half * 64 * 128 / 16);
-#pragma unroll
-              for (int s = 0; s < kKeys / 32; ++s)
-                umma_f16_ts(tmem + 256u + uint32_t(i * 128), tmem + uint32_t(i * 128 + half * 32 + 8 * s), b + uint64_t(16 * 128 / 16 * s), idesc_o,
-                            j != 0 || half != 0 || s != 0 ? 1u : 0u);
-              umma_commit(smem_u32(half ? &S.pv_done[i] : &S.pv_half[i]));
+            for (int s = 0; s < kSteps; ++s) {
+              const uint32_t off = uint32_t(s >> 2) * (128 * 128 / 16) + uint32_t(s & 3) * 2;
+              umma_f16(tmem + uint32_t(i * 128), a + off, b + off, idesc_s, s != 0 ? 1u : 0u);
             }
-            __syncwarp();
+            umma_commit(smem_u32(&S.s_full[i]));
+          }
+          __syncwarp();
+        };
+        // a step's keys: both tiles' S
+        auto keys_ready = [&]() {
+          ok = ok && wait_for(S.k_full[kg & 1], kg >> 1, abort, 103, P.status);
+          ok = __all_sync(0xffffffffu, ok);
+          tc_fence_after();
+          return ok;
+        };
+        if (!keys_ready()) break;
+#pragma unroll 1
+        for (int i = 0; i < 2 && ok; ++i) {
+          if (x.end[i] <= x.j0) continue;
+          ok = __all_sync(0xffffffffu, wait_for(S.q_full[i], ph_q >> i, abort, 104, P.status));
+          if (!ok) break;
+          ph_q ^= 1u << i;
+          tc_fence_after();
+          issue_s(i, kg & 1);
+        }
+        if (!ok) break;
+        if (issues) umma_commit(smem_u32(&S.k_empty[kg & 1]));
+        __syncwarp();
+        ++kg;
+#pragma unroll 1
+        for (int j = 0; j < n && ok; ++j, ++vg) {
+          const bool more = j + 1 < n;
+          if (j + 3 == n && lane == 0) mbar_arrive(smem_u32(&S.ask));
+          bool keys = false, values = false;
+#pragma unroll 1
+          for (int i = 0; i < 2; ++i) {
+            if (x.j0 + j >= x.end[i]) continue;
+            if (!values) { ok = wait_for(S.v_full[vg & 1], vg >> 1, abort, 106, P.status); values = true; }
+            if (ok && j == 0) ok = wait_for(S.o_empty[i], (ph_o >> i) ^ 1u, abort, 107, P.status);
+            // (the weights come in two halves)
+#pragma unroll 1
+            for (int half = 0; half < 2 && ok; ++half) {
+              ok = wait_for(S.p_full[i][half], ph_p >> i, abort, 105, P.status);
+              if (!(ok = __all_sync(0xffffffffu, ok))) break;
+              tc_fence_after();
+              if (issues) {
+                const uint64_t b = dv0 + uint64_t((vg & 1) * (Sh::kTile >> 4)) + uint64_t(half * 64 * 128 / 16);
+#pragma unroll 1
+                for (int s = 0; s < kKeys / 32; ++s)
+                  umma_f16_ts(tmem + 256u + uint32_t(i * 128), tmem + uint32_t(i * 128 + half * 32 + 8 * s), b + uint64_t(16 * 128 / 16 * s), idesc_o,
+                              j != 0 || half != 0 || s != 0 ? 1u : 0u);
+                umma_commit(smem_u32(half ? &S.pv_done[i] : &S.pv_half[i]));
+              }
+              __syncwarp();
+            }
+            if (!ok) break;
+            ph_p ^= 1u << i;
+            if (j == 0) ph_o ^= 1u << i;
+            if (x.j0 + j + 1 < x.end[i]) {
+              if (!keys) { if (!keys_ready()) break; keys = true; }
+              issue_s(i, kg & 1);
+            }
           }
           if (!ok) break;
-          ph_p ^= 1u << i;
-          if (j == 0) ph_o ^= 1u << i;
-          if (x.j0 + j + 1 < x.end[i]) {
-            if (!keys) { if (!keys_ready()) break; keys = true; }
-            issue_s(i, kg & 1);
+          if (issues) {
+            umma_commit(smem_u32(&S.v_empty[vg & 1]));
+            if (more) umma_commit(smem_u32(&S.k_empty[kg & 1]));
           }
+          __syncwarp();
+          if (more) ++kg;
         }
-        if (!ok) break;
-        if (issues) {
-          umma_commit(smem_u32(&S.v_empty[vg & 1]));
-          if (more) umma_commit(smem_u32(&S.k_empty[kg & 1]));
-        }
-        __syncwarp();
-        if (more) ++kg;
       }
-    }
-    if (issues) umma_commit(smem_u32(&S.done));
-    __syncwarp();
-    mbar_drain(smem_u32(&S.done), 0);
-  } else if (warp >= kSoftWarps && warp < kMmaWarp) {
+      if (issues) umma_commit(smem_u32(&S.done));
+      __syncwarp();
+      mbar_drain(smem_u32(&S.done), 0);
+  }
+  } else if (warp >= kSoftWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kConvRegs));
     // ---------------------------------------------------------------- codes to f16 tiles
     const int t = tid - 32 * kSoftWarps;
-    constexpr int kPer = kSteps;                          // pieces of 16 codes: 128 rows x kSteps over 128 threads
+    constexpr int kPer = kSteps;                          // pieces of 16 codes of a thread: 128 rows x kSteps over 128 threads
     const AttendParams& A = P.a;
     uint32_t kg = 0, vg = 0;
     bool ok = true;
@@ -458,91 +465,81 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
       if (n <= 0) continue;
       const int32_t* table = A.table + x.b * A.ld_table;
       const int seen = min(min(x.before + (min(x.row0 + kPair, x.n_rows) - 1) / A.group + 1, A.max_kv), int(min((long long)A.table_width << A.shift, (long long)INT32_MAX)));
-      // This thread's pieces of 16 codes.  Heads of 128 channels: eight neighbouring lanes take four pieces of two rows, whose places
-      // in the tile lie in different banks.
+      // This thread's pieces of 16 codes, copied and converted by itself.  Heads of 128 channels: eight neighbouring lanes take four
+      // pieces of two rows, whose places in the tile lie in different banks.
       auto row_at = [&](int i) { return kSteps == 8 ? i * 16 + ((t >> 4) << 1 | (t >> 2 & 1)) : (i * 128 + t) / kSteps; };
       auto piece_of = [&](int i) { return kSteps == 8 ? (t & 3) | (t >> 3 & 1) << 2 : (i * 128 + t) % kSteps; };
-      // where they lie in K and V, in units of 16 bytes; kNone: no such block
-      constexpr uint32_t kNone = 0xffffffffu;
-      uint32_t place[kPer];
-      int page[kPer];
+      // lanes 0 to 7 hold the blocks of a step's eight groups of 16 keys, of the step that is copied next
+      auto page_of = [&](int j) {
+        const int key = (x.j0 + j) * kKeys + 16 * (lane & 7);
+        int page = -1;
+        if (j < n && key < seen) asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(page) : "l"(table + (key >> A.shift)));
+        return page;
+      };
+      // in units of 16 bytes
       const uint32_t block_units = uint32_t(A.c.kv_heads * kSteps) << A.shift, head_units = uint32_t(x.h * kSteps) << A.shift;
-      auto pages_of = [&](int j) {
-#pragma unroll
+      auto fetch = [&](uint8_t* raw, const uint8_t* codes, int page) {
+#pragma unroll 2
         for (int i = 0; i < kPer; ++i) {
-          const int key = (x.j0 + j) * kKeys + row_at(i);
-          page[i] = -1;
-          if (j < n && key < seen) asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(page[i]) : "l"(table + (key >> A.shift)));
+          const int r = row_at(i), pg = __shfl_sync(0xffffffffu, page, r >> 4);
+          // (steps begin blocks; pieces of no block keep any bytes: their tokens weigh nothing)
+          if (unsigned(pg) < unsigned(A.c.num_blocks)) {
+            const uint32_t at = uint32_t(pg) * block_units + head_units + uint32_t((r & ((1 << A.shift) - 1)) * kSteps + piece_of(i));
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(raw) + uint32_t(i * 128 + t) * 16u), "l"(codes + uint64_t(at) * 16) : "memory");
+          }
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
       };
-      auto places = [&]() {                               // (steps begin blocks)
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-          place[i] = unsigned(page[i]) < unsigned(A.c.num_blocks)
-                         ? uint32_t(page[i]) * block_units + head_units + uint32_t((row_at(i) & ((1 << A.shift) - 1)) * kSteps + piece_of(i))
-                         : kNone;
-      };
-      // Codes are asked for a step ahead: K and V of it are in flight while this step's are converted.  (Pieces of no block keep any bytes:
-      // their tokens weigh nothing.)
-      uint4 raw_k[kPer] = {}, raw_v[kPer] = {};
-      auto fetch = [&](uint4 (&raw)[kPer], const uint8_t* codes) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-          // (volatile: the compiler would otherwise move the load down to its use)
-          if (place[i] != kNone)
-            asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];"
-                         : "+r"(raw[i].x), "+r"(raw[i].y), "+r"(raw[i].z), "+r"(raw[i].w) : "l"(codes + uint64_t(place[i]) * 16));
-      };
-      auto convert = [&](const uint4 (&raw)[kPer], uint8_t* tile, bool k) {
+      auto convert = [&](const uint8_t* raw, uint8_t* tile, bool k) {
         auto lo = [&](uint32_t w) { return k ? bf16_codes(w, 0x4140) : codes_lo(w); };
         auto hi = [&](uint32_t w) { return k ? bf16_codes(w, 0x4342) : codes_hi(w); };
-#pragma unroll
+#pragma unroll 2
         for (int i = 0; i < kPer; ++i) {
           const int r = row_at(i), p = piece_of(i);
-          *reinterpret_cast<uint4*>(tile + piece_at(r, 2 * p)) = make_uint4(lo(raw[i].x), hi(raw[i].x), lo(raw[i].y), hi(raw[i].y));
-          *reinterpret_cast<uint4*>(tile + piece_at(r, 2 * p + 1)) = make_uint4(lo(raw[i].z), hi(raw[i].z), lo(raw[i].w), hi(raw[i].w));
+          const uint4 c = *reinterpret_cast<const uint4*>(raw + (i * 128 + t) * 16);
+          *reinterpret_cast<uint4*>(tile + piece_at(r, 2 * p)) = make_uint4(lo(c.x), hi(c.x), lo(c.y), hi(c.y));
+          *reinterpret_cast<uint4*>(tile + piece_at(r, 2 * p + 1)) = make_uint4(lo(c.z), hi(c.z), lo(c.w), hi(c.w));
         }
         fence_async_smem();
         __syncwarp();
       };
-      // the scales of eight groups of 16 keys
-      float ks = 0.f, vs = 0.f;                           // (0: no block; its tokens weigh nothing)
-      auto fetch_scales = [&](int j) {
+      // the scales of the groups (0: no block; its tokens weigh nothing)
+      float ks = 0.f, vs = 0.f;
+      int page = page_of(0);
+#pragma unroll 1
+      for (int j = -1; j < n; ++j) {
+        if (j >= 0) {
+          asm volatile("cp.async.wait_group 1;" ::: "memory");                 // (K of this step; its V may be on its way)
+          if (!(ok = __all_sync(0xffffffffu, wait_for(S.k_empty[kg & 1], (kg >> 1) ^ 1u, abort, 108, P.status)))) break;
+          if (t < 8) S.scale[kg & 3][t] = vs > 0.f ? make_float4(ks, lg2(vs), __fdividef(1.f, vs), 0.f) : make_float4(1.f, -CUDART_INF_F, 0.f, 0.f);
+          convert(S.raw[0], S.k[kg & 1], true);
+          if (lane == 0) mbar_arrive(smem_u32(&S.k_full[kg & 1]));
+          ++kg;
+        }
+        const int now = page;
+        fetch(S.raw[0], A.c.k_codes, now);                // (past the last step: no blocks, nothing is copied)
         if (t < 8) {
-          const int key = (x.j0 + j) * kKeys + 16 * t;
-          const int pg = j < n && key < seen ? __ldg(table + (key >> A.shift)) : -1;
           vs = 0.f;
-          if (unsigned(pg) < unsigned(A.c.num_blocks)) {
-            const int64_t at = int64_t(pg) * A.c.kv_heads + x.h;
+          if (unsigned(now) < unsigned(A.c.num_blocks)) {
+            const int64_t at = int64_t(now) * A.c.kv_heads + x.h;
             asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(ks) : "l"(A.c.k_scale + at));
             asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(vs) : "l"(A.c.v_scale + at));
           }
         }
-      };
-      pages_of(0);
-#pragma unroll 1
-      for (int j = -1; j < n; ++j) {
+        page = page_of(j + 2);
         if (j >= 0) {
-          if (!(ok = __all_sync(0xffffffffu, wait_for(S.k_empty[kg & 1], (kg >> 1) ^ 1u, abort, 108, P.status)))) break;
-          if (t < 8) S.scale[kg & 3][t] = vs > 0.f ? make_float4(ks, lg2(vs), __fdividef(1.f, vs), 0.f) : make_float4(1.f, -CUDART_INF_F, 0.f, 0.f);
-          convert(raw_k, S.k[kg & 1], true);
-          if (lane == 0) mbar_arrive(smem_u32(&S.k_full[kg & 1]));
-          ++kg;
-        }
-        places();
-        fetch(raw_k, A.c.k_codes);                        // (past the last step: no places, nothing is read)
-        fetch_scales(j + 1);
-        if (j >= 0) {
+          asm volatile("cp.async.wait_group 1;" ::: "memory");                 // (V of this step; the next one's K may be on its way)
           if (!(ok = __all_sync(0xffffffffu, wait_for(S.v_empty[vg & 1], (vg >> 1) ^ 1u, abort, 109, P.status)))) break;
-          convert(raw_v, S.v[vg & 1], false);
+          convert(S.raw[1], S.v[vg & 1], false);
           if (lane == 0) mbar_arrive(smem_u32(&S.v_full[vg & 1]));
           ++vg;
         }
-        fetch(raw_v, A.c.v_codes);
-        pages_of(j + 2);
+        fetch(S.raw[1], A.c.v_codes, now);
       }
+      asm volatile("cp.async.wait_all;" ::: "memory");
     }
-  } else if (warp < kSoftWarps) {
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     // ---------------------------------------------------------------- softmax, a thread per row
     const AttendParams& A = P.a;
     const int i = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
@@ -603,33 +600,45 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
         tc_fence_after();
         const bool masked = __any_sync(0xffffffffu, sees < kKeys);
         const float4* scale = S.scale[(kg + j) & 3];
-        // 32 keys: exponents on the m so far, and the columns' maximum beside them; if it turns out too far above m, m moves and
-        // the columns are read again
-        auto group = [&](uint32_t (&s)[32], int c) {
-          const float4 g0 = scale[2 * c], g1 = scale[2 * c + 1];
-          const float f0 = g0.x * A.scale, f1 = g1.x * A.scale;
+        // 64 keys at a time: exponents on the m so far, and the columns' maximum beside them; if it turns out too far above m, m moves
+        // and the columns are read again
+        uint32_t s[2][32];
+        tmem_ld32(t_s, s[0]);
+        tmem_ld32(t_s + 32u, s[1]);
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          float4 g[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            g[k] = scale[4 * half + k];
+            g[k].x *= A.scale;
+          }
 #pragma unroll 1
           for (;;) {
-            tmem_ld_wait32(s);
+            tmem_ld_wait32(s[0]);
+            tmem_ld_wait32(s[1]);
             if (masked) {
 #pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (32 * c + e >= sees) s[e] = 0xff800000u;
+              for (int e = 0; e < 64; ++e)
+                if (64 * half + e >= sees) s[e >> 5][e & 31] = 0xff800000u;
             }
-            float t0 = __uint_as_float(s[0]), t1 = __uint_as_float(s[16]);
+            float top = -CUDART_INF_F;
 #pragma unroll
-            for (int e = 1; e < 15; e += 2) {
-              t0 = max3(t0, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-              t1 = max3(t1, __uint_as_float(s[16 + e]), __uint_as_float(s[17 + e]));
-            }
-            const float top = fmaxf(fmaf(fmaxf(t0, __uint_as_float(s[15])), f0, g0.y), fmaf(fmaxf(t1, __uint_as_float(s[31])), f1, g1.y));
-            const f32x2 ff0 = splat2(f0), ff1 = splat2(f1), b0 = splat2(base + g0.y), b1 = splat2(base + g1.y);
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t* v = &s[k >> 1][16 * (k & 1)];
+              float t = __uint_as_float(v[0]);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              float a, b;
-              unpack2(fma2(pack2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), e < 8 ? ff0 : ff1, e < 8 ? b0 : b1), a, b);
-              s[2 * e] = __float_as_uint(ex2(a));
-              s[2 * e + 1] = __float_as_uint(ex2(b));
+              for (int e = 1; e < 15; e += 2) t = max3(t, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
+              top = fmaxf(top, fmaf(fmaxf(t, __uint_as_float(v[15])), g[k].x, g[k].y));
+              const f32x2 f = splat2(g[k].x), b = splat2(base + g[k].y);
+              uint32_t* o = &s[k >> 1][16 * (k & 1)];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                float lo, hi;
+                unpack2(fma2(pack2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), f, b), lo, hi);
+                o[2 * e] = __float_as_uint(ex2(lo));
+                o[2 * e + 1] = __float_as_uint(ex2(hi));
+              }
             }
             if (!__any_sync(0xffffffffu, top > m + kLag)) break;
             // m rises: what has been summed and written so far is brought down
@@ -638,43 +647,36 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
             z *= down;
             m = up;
             base = m == -CUDART_INF_F ? 0.f : kLift - m;
-            if (j > 0 || c >= 2) {
-              // the accumulator, once it has the weights handed over so far: the step before's, or this step's first half
-              ok = c < 2 ? wait_for(S.pv_done[i], ph_pv ^ 1u, abort, 111, P.status) : wait_for(S.pv_half[i], ph_pv, abort, 114, P.status);
-              if (!(ok = __all_sync(0xffffffffu, ok))) break;
-              tc_fence_after();
+            // (the accumulator has, or will have, what was handed over: the step before's weights, or this step's first half)
+            if (j > 0 || half > 0) {
+              if (!(ok = bring_down(half == 0 ? S.pv_done[i] : S.pv_half[i], half == 0 ? ph_pv ^ 1u : ph_pv, abort, P.status, t_o, kSteps, down))) break;
             }
-            bring_down(t_s, c & ~1, c, t_o, j > 0 || c >= 2 ? kSteps : 0, down);     // (weights that have not been handed over)
-            tmem_ld32(t_s + 32u * c, s);
+            tmem_ld32(t_s + 64u * half, s[0]);
+            tmem_ld32(t_s + 64u * half + 32u, s[1]);
           }
-          f32x2 sum0 = splat2(0.f), sum1 = splat2(0.f);
-          uint32_t w[16];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float a = __uint_as_float(s[2 * e]), b = __uint_as_float(s[2 * e + 1]);
-            if (e < 8) sum0 = add2(sum0, pack2(a, b)); else sum1 = add2(sum1, pack2(a, b));
-            w[e] = bits_of(__floats2half2_rn(a, b));
-          }
-          if (c < 3) tmem_ld32(t_s + 32u * (c + 1), s);
-          tmem_st16(t_s + 16u * c, w);
-          float a, b;
-          unpack2(sum0, a, b);
-          z = fmaf(a + b, g0.z, z);
-          unpack2(sum1, a, b);
-          z = fmaf(a + b, g1.z, z);
-        };
-        uint32_t s[32];
-        tmem_ld32(t_s, s);
-#pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
-          group(s, c);
           if (!ok) break;
-          if (c & 1) {
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&S.p_full[i][c >> 1]));
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            f32x2 sum0 = splat2(0.f), sum1 = splat2(0.f);
+            uint32_t w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float a = __uint_as_float(s[q][2 * e]), b = __uint_as_float(s[q][2 * e + 1]);
+              if (e < 8) sum0 = add2(sum0, pack2(a, b)); else sum1 = add2(sum1, pack2(a, b));
+              w[e] = bits_of(__floats2half2_rn(a, b));
+            }
+            if (half == 0) tmem_ld32(t_s + 64u + 32u * q, s[q]);
+            tmem_st16(t_s + 32u * half + 16u * q, w);
+            float a, b;
+            unpack2(sum0, a, b);
+            z = fmaf(a + b, g[2 * q].z, z);
+            unpack2(sum1, a, b);
+            z = fmaf(a + b, g[2 * q + 1].z, z);
           }
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&S.p_full[i][half]));
         }
         if (!ok) break;
         sees -= kKeys;
@@ -711,42 +713,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
         if (writes) __threadfence();
       }
       if (writes) {
-        float2 mz = make_float2(m, z);
-        if (A.out_kind == REPQ_OUT_BF16 && parts == 1) {
-          // 64 channels at a time through shared memory: a store of the warp then covers whole rows, not 16 bytes of 32
-          const float inv = z > 0.f ? __fdividef(1.f, z) : z == 0.f ? 0.f : CUDART_NAN_F;
-          uint8_t* stage = S.stage[warp];
-          const long long off = row.in ? row.token * A.ldo + row.head * A.o_sh : -1;
-#pragma unroll 1
-          for (int b0 = 0; b0 < kSteps; b0 += kStage) {
-#pragma unroll 1
-            for (int b = 0; b < kStage; ++b) {
-              uint32_t w[16] = {};
-              if (n > 0) {
-                tmem_ld16(t_o + 16u * (b0 + b), w);
-                tmem_ld_wait(w);
-              }
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(w[2 * e]) * inv, __uint_as_float(w[2 * e + 1]) * inv);
-                w[e] = *reinterpret_cast<const uint32_t*>(&h);
-              }
-              *reinterpret_cast<uint4*>(stage + lane * 128 + (((2 * b) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-              *reinterpret_cast<uint4*>(stage + lane * 128 + (((2 * b + 1) ^ (lane & 7)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
-            }
-            __syncwarp();
-#pragma unroll 2
-            for (int e = lane; e < 32 * 2 * kStage; e += 32) {
-              const int rr = e / (2 * kStage), c = e - rr * (2 * kStage);
-              const long long at = __shfl_sync(0xffffffffu, off, rr);
-              const uint4 w = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((c ^ (rr & 7)) << 4));
-              if (at >= 0) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(A.out) + at + 16 * b0 + 8 * c) = w;
-            }
-            __syncwarp();
-          }
-        } else {
-          mz = put_row<kSteps>(A, row, r, t_o, n > 0, m, z, parts0, parts);
-        }
+        const float2 mz = put_row<kSteps>(A, row, r, t_o, n > 0, m, z, parts0, parts);
         if (row.in && A.lse)
           A.lse[int64_t(row.token) * A.heads + row.head] = mz.y > 0.f ? (mz.x - kLift + log2f(mz.y)) * kLn2 : mz.y == 0.f ? -CUDART_INF_F : CUDART_NAN_F;
       }
