@@ -1,10 +1,11 @@
 // Attention over the 8-bit cache for chunks of prompts: many rows per key / value head, on tcgen05.
 //
-// A CTA takes 256 rows of one key / value head of a request (token x group) as two tiles of 128, and walks the keys they see in steps
-// of 128.  Four warps turn the codes of a step into tiles of shared memory (code - 128 is exact in either type): K in bf16, as the queries
-// are, V in f16 as the MN-major operand of the same layout.  Per tile S = Q K^T goes to 128 columns of tensor memory; a thread per row
-// forms weights 32 columns at a time and writes them, f16, over columns it has read, from where O += P V takes them.  The two
-// tiles alternate: one's softmax runs under the other's MMAs.
+// A CTA takes 256 rows of one key / value head of a request (token x group) as two tiles of 128, and walks the keys they see.  Four warps
+// turn the codes of 128 keys at a time into tiles of shared memory (code - 128 is exact in either type): K in bf16, as the queries are, V in
+// f16 as the MN-major operand of the same layout.  A tile takes 64 keys at a time: S = Q K^T goes to one of two halves of its 128
+// columns of tensor memory, two steps ahead of the softmax; a thread per row forms the weights of a half and writes them, f16, over
+// its columns, from where O += P V takes them.  So neither the softmax nor the MMAs wait for each other's last step (128 keys at
+// a time and S behind the product: a third of the time went by in such waits).
 //
 // With x = S alpha k_scale log2 e and lv = log2 v_scale, both per 16 keys, weights are w = 2^(x + lv - m + 7): the value scales go into the exponent, so no product per key is spent on them, and
 // the sum is Z = sum w / v_scale, a product per 16 keys.  m follows the largest x + lv of the row at a distance of up to 8, so w
@@ -27,7 +28,8 @@ namespace chunks {
 
 using namespace tc;
 
-constexpr int kTileRows = 128, kPair = 2 * kTileRows, kKeys = 128;
+constexpr int kTileRows = 128, kPair = 2 * kTileRows;
+constexpr int kKeys = 128, kHalf = 64;   // keys that are converted at a time, and that a tile takes at a time
 constexpr int kSoftWarps = 8, kConvWarps = 4;
 constexpr int kMmaWarp = kSoftWarps + kConvWarps, kItemWarp = kMmaWarp + 1;
 constexpr int kThreads = 512;             // (two warps of the last group have nothing to do)
@@ -36,7 +38,8 @@ constexpr int kSoftRegs = 176, kConvRegs = 80, kOtherRegs = 80;
 constexpr float kLift = 7.f, kLag = 8.f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-struct Item { int b, h, row0, q0, before, n_rows, j0, end[2], part, id; };   // before: tokens ahead of the request's first query
+// before: tokens ahead of the request's first query; j0: its first step of 128 keys; ends: steps of 64 keys of its two tiles, from there
+struct Item { int b, h, row0, q0, before, n_rows, j0, ends[2], part, id; };
 
 struct ChunkParams {
   AttendParams a;
@@ -56,7 +59,7 @@ struct Shared {
   float4 scale[4][8];                    // per step (four in turn) and 16 keys: k_scale, log2 v_scale, 1 / v_scale
   Item item[2];
   int items, last[2];
-  alignas(8) uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], p_full[2][2], pv_half[2], pv_done[2], o_empty[2], item_full[2],
+  alignas(8) uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2][2], p_full[2][2], pv_done[2][2], o_empty[2], item_full[2],
       item_empty[2], ask, done;
   uint32_t tmem_base;
   volatile int abort;
@@ -235,11 +238,12 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
       mbar_init(smem_u32(&S.v_full[i]), kConvWarps);
       mbar_init(smem_u32(&S.v_empty[i]), 1);
       mbar_init(smem_u32(&S.q_full[i]), 4);
-      mbar_init(smem_u32(&S.s_full[i]), 1);
+      mbar_init(smem_u32(&S.s_full[i][0]), 1);
+      mbar_init(smem_u32(&S.s_full[i][1]), 1);
       mbar_init(smem_u32(&S.p_full[i][0]), 4);
       mbar_init(smem_u32(&S.p_full[i][1]), 4);
-      mbar_init(smem_u32(&S.pv_half[i]), 1);
-      mbar_init(smem_u32(&S.pv_done[i]), 1);
+      mbar_init(smem_u32(&S.pv_done[i][0]), 1);
+      mbar_init(smem_u32(&S.pv_done[i][1]), 1);
       mbar_init(smem_u32(&S.o_empty[i]), 4);
       mbar_init(smem_u32(&S.item_full[i]), 1);
       mbar_init(smem_u32(&S.item_empty[i]), kSoftWarps + kConvWarps + 1);
@@ -331,18 +335,17 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
           x.q0 = rq.q0;
           x.before = rq.kv - rq.q_true;
           x.n_rows = rq.q_len * P.a.group;
-          int steps[2], most = 0;
+          int seen[2];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const int rows = min(x.n_rows - x.row0 - i * kTileRows, kTileRows);
-            const int seen = rows > 0 ? min(min(x.before + (x.row0 + i * kTileRows + rows - 1) / P.a.group + 1, rq.kv), P.a.max_kv) : 0;
-            steps[i] = seen > 0 ? (seen + kKeys - 1) / kKeys : 0;
-            most = max(most, steps[i]);
+            seen[i] = rows > 0 ? max(min(min(x.before + (x.row0 + i * kTileRows + rows - 1) / P.a.group + 1, rq.kv), P.a.max_kv), 0) : 0;
           }
+          const int most = (max(seen[0], seen[1]) + kKeys - 1) / kKeys;
           x.j0 = int((long long)most * x.part / parts);
           const int j1 = int((long long)most * (x.part + 1) / parts);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) x.end[i] = max(min(steps[i], j1), x.j0);
+          for (int i = 0; i < 2; ++i) x.ends[i] = max(min((seen[i] + kHalf - 1) / kHalf, 2 * j1) - 2 * x.j0, 0);
         }
         if (lane == 0) {
           S.item[it & 1] = x;
@@ -358,94 +361,99 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
     } else if (warp == kMmaWarp) {
       // ---------------------------------------------------------------- MMAs
       const bool issues = elect_one();
-      // D = f32; S: A and B bf16, K-major, N = 128; P V: f16, A in tensor memory, B MN-major, N = d_h
-      constexpr uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(kKeys >> 3) << 17) | (uint32_t(kTileRows >> 4) << 24);
+      // D = f32; S: A and B bf16, K-major, N = 64; P V: f16, A in tensor memory, B MN-major, N = d_h
+      constexpr uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(kHalf >> 3) << 17) | (uint32_t(kTileRows >> 4) << 24);
       constexpr uint32_t idesc_o = (1u << 4) | (1u << 16) | (uint32_t(dh >> 3) << 17) | (uint32_t(kTileRows >> 4) << 24);
       const uint64_t dq0 = smem_desc_sw128(smem_u32(S.q[0])), dk0 = smem_desc_sw128(smem_u32(S.k[0])),
                      dv0 = smem_desc_sw128(smem_u32(S.v[0]), 128 * 128);
-      uint32_t kg = 0, vg = 0;                              // steps of K and V taken
-      uint32_t ph_q = 0, ph_p = 0, ph_o = 0;                // a bit per tile
+      uint32_t g = 0;                                     // steps of 128 keys taken before this item
+      uint32_t ph_q = 0, ph_p = 0, ph_o = 0;              // a bit per tile (ph_p: per tile and half)
       bool ok = true;
       Item x;
       for (int it = 0; ok && next_item(it, x); ++it) {
-        const int n = max(x.end[0], x.end[1]) - x.j0;
-        if (n <= 2 && lane == 0) mbar_arrive(smem_u32(&S.ask));
+        // (steps of 64 keys; told as alike for all lanes: descriptors then stay in uniform registers, from which MMAs take them.  Moved there
+        // one by one they took 150 cycles an MMA.)
+        const int ends[2] = {__shfl_sync(0xffffffffu, x.ends[0], 0), __shfl_sync(0xffffffffu, x.ends[1], 0)};
+        const int n = max(ends[0], ends[1]);
+        if (n <= 6 && lane == 0) mbar_arrive(smem_u32(&S.ask));
         if (n <= 0) continue;
-        auto issue_s = [&](int i, uint32_t slot) {
-          if (issues) {
-            const uint64_t a = dq0 + uint64_t(i * (Sh::kTile >> 4)), b = dk0 + uint64_t(slot * (Sh::kTile >> 4));
-#pragma unroll 1
-            for (int s = 0; s < kSteps; ++s) {
-              const uint32_t off = uint32_t(s >> 2) * (128 * 128 / 16) + uint32_t(s & 3) * 2;
-              umma_f16(tmem + uint32_t(i * 128), a + off, b + off, idesc_s, s != 0 ? 1u : 0u);
-            }
-            umma_commit(smem_u32(&S.s_full[i]));
+        int k_there = -1, v_there = -1;                   // steps of 128 whose tiles have been waited for
+        auto keys = [&](int u) {
+          if ((u >> 1) > k_there) {
+            const uint32_t at = g + uint32_t(u >> 1);
+            ok = __all_sync(0xffffffffu, wait_for(S.k_full[at & 1], at >> 1, abort, 103, P.status));
+            k_there = u >> 1;
+            tc_fence_after();
           }
-          __syncwarp();
-        };
-        // a step's keys: both tiles' S
-        auto keys_ready = [&]() {
-          ok = ok && wait_for(S.k_full[kg & 1], kg >> 1, abort, 103, P.status);
-          ok = __all_sync(0xffffffffu, ok);
-          tc_fence_after();
           return ok;
         };
-        if (!keys_ready()) break;
-#pragma unroll 1
-        for (int i = 0; i < 2 && ok; ++i) {
-          if (x.end[i] <= x.j0) continue;
-          ok = __all_sync(0xffffffffu, wait_for(S.q_full[i], ph_q >> i, abort, 104, P.status));
-          if (!ok) break;
-          ph_q ^= 1u << i;
-          tc_fence_after();
-          issue_s(i, kg & 1);
-        }
-        if (!ok) break;
-        if (issues) umma_commit(smem_u32(&S.k_empty[kg & 1]));
-        __syncwarp();
-        ++kg;
-#pragma unroll 1
-        for (int j = 0; j < n && ok; ++j, ++vg) {
-          const bool more = j + 1 < n;
-          if (j + 3 == n && lane == 0) mbar_arrive(smem_u32(&S.ask));
-          bool keys = false, values = false;
-#pragma unroll 1
-          for (int i = 0; i < 2; ++i) {
-            if (x.j0 + j >= x.end[i]) continue;
-            if (!values) { ok = wait_for(S.v_full[vg & 1], vg >> 1, abort, 106, P.status); values = true; }
-            if (ok && j == 0) ok = wait_for(S.o_empty[i], (ph_o >> i) ^ 1u, abort, 107, P.status);
-            // (the weights come in two halves)
-#pragma unroll 1
-            for (int half = 0; half < 2 && ok; ++half) {
-              ok = wait_for(S.p_full[i][half], ph_p >> i, abort, 105, P.status);
-              if (!(ok = __all_sync(0xffffffffu, ok))) break;
-              tc_fence_after();
-              if (issues) {
-                const uint64_t b = dv0 + uint64_t((vg & 1) * (Sh::kTile >> 4)) + uint64_t(half * 64 * 128 / 16);
-#pragma unroll 1
-                for (int s = 0; s < kKeys / 32; ++s)
-                  umma_f16_ts(tmem + 256u + uint32_t(i * 128), tmem + uint32_t(i * 128 + half * 32 + 8 * s), b + uint64_t(16 * 128 / 16 * s), idesc_o,
-                              j != 0 || half != 0 || s != 0 ? 1u : 0u);
-                umma_commit(smem_u32(half ? &S.pv_done[i] : &S.pv_half[i]));
-              }
-              __syncwarp();
-            }
-            if (!ok) break;
-            ph_p ^= 1u << i;
-            if (j == 0) ph_o ^= 1u << i;
-            if (x.j0 + j + 1 < x.end[i]) {
-              if (!keys) { if (!keys_ready()) break; keys = true; }
-              issue_s(i, kg & 1);
-            }
-          }
-          if (!ok) break;
+        // S of step u into the half of the tile's columns whose weights the product of step u - 2 has taken
+        auto issue_s = [&](int i, int u) {
           if (issues) {
-            umma_commit(smem_u32(&S.v_empty[vg & 1]));
-            if (more) umma_commit(smem_u32(&S.k_empty[kg & 1]));
+            const uint64_t a = dq0 + uint64_t(i * (Sh::kTile >> 4));
+            const uint64_t b = dk0 + uint64_t(((g + uint32_t(u >> 1)) & 1) * (Sh::kTile >> 4)) + uint64_t((u & 1) * (kHalf * 128 / 16));
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+              const uint32_t off = uint32_t(s >> 2) * (128 * 128 / 16) + uint32_t(s & 3) * 2;
+              umma_f16(tmem + uint32_t(i * 128 + (u & 1) * 64), a + off, b + off, idesc_s, s != 0 ? 1u : 0u);
+            }
+            umma_commit(smem_u32(&S.s_full[i][u & 1]));
           }
           __syncwarp();
-          if (more) ++kg;
+        };
+        auto keys_read = [&](int u) {                     // both tiles' S of step u are issued
+          if (issues && ((u & 1) || u + 1 == n)) umma_commit(smem_u32(&S.k_empty[(g + uint32_t(u >> 1)) & 1]));
+          __syncwarp();
+        };
+#pragma unroll 1
+        for (int u = 0; u < min(n, 2) && ok; ++u) {
+          if (!keys(u)) break;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (u >= ends[i]) continue;
+            if (u == 0) {
+              if (!(ok = __all_sync(0xffffffffu, wait_for(S.q_full[i], ph_q >> i, abort, 104, P.status)))) break;
+              ph_q ^= 1u << i;
+              tc_fence_after();
+            }
+            issue_s(i, u);
+          }
+          if (ok) keys_read(u);
         }
+#pragma unroll 1
+        for (int u = 0; u < n && ok; ++u) {
+          if (u + 6 == n && lane == 0) mbar_arrive(smem_u32(&S.ask));
+          const uint32_t at = g + uint32_t(u >> 1);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (u >= ends[i]) continue;
+            if ((u >> 1) > v_there) { ok = wait_for(S.v_full[at & 1], at >> 1, abort, 106, P.status); v_there = u >> 1; }
+            if (ok && u == 0) { ok = wait_for(S.o_empty[i], (ph_o >> i) ^ 1u, abort, 107, P.status); ph_o ^= 1u << i; }
+            const int slot = 2 * i + (u & 1);
+            ok = ok && wait_for(S.p_full[i][u & 1], ph_p >> slot, abort, 105, P.status);
+            if (!(ok = __all_sync(0xffffffffu, ok))) break;
+            ph_p ^= 1u << slot;
+            tc_fence_after();
+            if (issues) {
+              const uint64_t b = dv0 + uint64_t((at & 1) * (Sh::kTile >> 4)) + uint64_t((u & 1) * (kHalf * 128 / 16));
+#pragma unroll
+              for (int s = 0; s < kHalf / 16; ++s)
+                umma_f16_ts(tmem + 256u + uint32_t(i * 128), tmem + uint32_t(i * 128 + (u & 1) * 64 + 8 * s), b + uint64_t(16 * 128 / 16 * s), idesc_o,
+                            u != 0 || s != 0 ? 1u : 0u);
+              umma_commit(smem_u32(&S.pv_done[i][u & 1]));
+            }
+            __syncwarp();
+            if (u + 2 < ends[i]) {
+              if (!keys(u + 2)) break;
+              issue_s(i, u + 2);
+            }
+          }
+          if (!ok) break;
+          if (u + 2 < n) keys_read(u + 2);
+          if (issues && ((u & 1) || u + 1 == n)) umma_commit(smem_u32(&S.v_empty[at & 1]));
+          __syncwarp();
+        }
+        g += uint32_t((n + 1) >> 1);
       }
       if (issues) umma_commit(smem_u32(&S.done));
       __syncwarp();
@@ -461,7 +469,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
     bool ok = true;
     Item x;
     for (int it = 0; ok && next_item(it, x); ++it) {
-      const int n = max(x.end[0], x.end[1]) - x.j0;
+      const int n = (max(x.ends[0], x.ends[1]) + 1) >> 1;
       if (n <= 0) continue;
       const int32_t* table = A.table + x.b * A.ld_table;
       const int seen = min(min(x.before + (min(x.row0 + kPair, x.n_rows) - 1) / A.group + 1, A.max_kv), int(min((long long)A.table_width << A.shift, (long long)INT32_MAX)));
@@ -545,7 +553,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
     const int i = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
     const uint32_t lanes = uint32_t(quarter * 32) << 16;
     const uint32_t t_s = tmem + lanes + uint32_t(i * 128), t_o = tmem + lanes + 256u + uint32_t(i * 128);
-    uint32_t ph_s = 0, ph_pv = 0;                         // phases waited for
+    uint32_t ph_s = 0, ph_pv = 0;                         // phases waited for, a bit per half (S is two steps ahead of the product: one
+                                                          // barrier would be two phases behind)
     uint32_t kg = 0;                                      // steps of K in all items (both tiles count alike)
     auto tile_barrier = [&]() {                           // of the tile's four warps
       if (i == 0) asm volatile("bar.sync 1, 128;" ::: "memory");
@@ -584,117 +593,108 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
     };
     bool ok = true;
     bool more = see_item(0);
-    if (more && S.item[0].end[i] > S.item[0].j0) { ask_q(S.item[0]); give_q(); }
+    if (more && S.item[0].ends[i] > 0) { ask_q(S.item[0]); give_q(); }
     for (int it = 0; more; ++it) {
       const volatile Item& x = S.item[it & 1];
-      const int n = x.end[i] - x.j0;
+      const int n = x.ends[i];                            // steps of 64 keys
       int sees = 0;                                       // keys that the row sees, from the item's first on
       {
         const OutRow row = row_of(x);
         if (row.in) sees = min(x.before + row.token - x.q0 + 1, A.max_kv) - x.j0 * kKeys;
       }
       float m = -CUDART_INF_F, z = 0.f, base = 0.f;       // base: kLift - m, 0 where nothing has been seen
-      for (int j = 0; j < n; ++j) {
-        if (!(ok = __all_sync(0xffffffffu, wait_for(S.s_full[i], ph_s, abort, 110, P.status)))) break;
-        ph_s ^= 1u;
-        tc_fence_after();
-        const bool masked = __any_sync(0xffffffffu, sees < kKeys);
-        const float4* scale = S.scale[(kg + j) & 3];
-        // 64 keys at a time: exponents on the m so far, and the columns' maximum beside them; if it turns out too far above m, m moves
-        // and the columns are read again
-        uint32_t s[2][32];
-        tmem_ld32(t_s, s[0]);
-        tmem_ld32(t_s + 32u, s[1]);
 #pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-          float4 g[4];
+      for (int u = 0; u < n; ++u) {
+        const int half = u & 1;
+        if (!(ok = __all_sync(0xffffffffu, wait_for(S.s_full[i][half], ph_s >> half, abort, 110, P.status)))) break;
+        ph_s ^= 1u << half;
+        tc_fence_after();
+        const bool masked = __any_sync(0xffffffffu, sees < kHalf);
+        const uint32_t t_u = t_s + 64u * half;
+        float4 g[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          g[k] = S.scale[(kg + uint32_t(u >> 1)) & 3][4 * half + k];
+          g[k].x *= A.scale;
+        }
+        // Exponents on the m so far, and the columns' maximum beside them; if it turns out too far above m, m moves and the columns are
+        // read again.
+        uint32_t s[2][32];
+#pragma unroll 1
+        for (;;) {
+          tmem_ld32(t_u, s[0]);
+          tmem_ld32(t_u + 32u, s[1]);
+          tmem_ld_wait32(s[0]);
+          tmem_ld_wait32(s[1]);
+          if (masked) {
+#pragma unroll
+            for (int e = 0; e < 64; ++e)
+              if (e >= sees) s[e >> 5][e & 31] = 0xff800000u;
+          }
+          float top = -CUDART_INF_F;
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            g[k] = scale[4 * half + k];
-            g[k].x *= A.scale;
+            uint32_t* v = &s[k >> 1][16 * (k & 1)];
+            float t = __uint_as_float(v[0]);
+#pragma unroll
+            for (int e = 1; e < 15; e += 2) t = max3(t, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
+            top = fmaxf(top, fmaf(fmaxf(t, __uint_as_float(v[15])), g[k].x, g[k].y));
+            const f32x2 f = splat2(g[k].x), b = splat2(base + g[k].y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              float lo, hi;
+              unpack2(fma2(pack2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), f, b), lo, hi);
+              v[2 * e] = __float_as_uint(ex2(lo));
+              v[2 * e + 1] = __float_as_uint(ex2(hi));
+            }
           }
-#pragma unroll 1
-          for (;;) {
-            tmem_ld_wait32(s[0]);
-            tmem_ld_wait32(s[1]);
-            if (masked) {
-#pragma unroll
-              for (int e = 0; e < 64; ++e)
-                if (64 * half + e >= sees) s[e >> 5][e & 31] = 0xff800000u;
-            }
-            float top = -CUDART_INF_F;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t* v = &s[k >> 1][16 * (k & 1)];
-              float t = __uint_as_float(v[0]);
-#pragma unroll
-              for (int e = 1; e < 15; e += 2) t = max3(t, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
-              top = fmaxf(top, fmaf(fmaxf(t, __uint_as_float(v[15])), g[k].x, g[k].y));
-              const f32x2 f = splat2(g[k].x), b = splat2(base + g[k].y);
-              uint32_t* o = &s[k >> 1][16 * (k & 1)];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                float lo, hi;
-                unpack2(fma2(pack2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), f, b), lo, hi);
-                o[2 * e] = __float_as_uint(ex2(lo));
-                o[2 * e + 1] = __float_as_uint(ex2(hi));
-              }
-            }
-            if (!__any_sync(0xffffffffu, top > m + kLag)) break;
-            // m rises: what has been summed and written so far is brought down
-            const float up = top > m + kLag ? top : m;
-            const float down = m == -CUDART_INF_F ? 0.f : ex2(m - up);
-            z *= down;
-            m = up;
-            base = m == -CUDART_INF_F ? 0.f : kLift - m;
-            // (the accumulator has, or will have, what was handed over: the step before's weights, or this step's first half)
-            if (j > 0 || half > 0) {
-              if (!(ok = bring_down(half == 0 ? S.pv_done[i] : S.pv_half[i], half == 0 ? ph_pv ^ 1u : ph_pv, abort, P.status, t_o, kSteps, down))) break;
-            }
-            tmem_ld32(t_s + 64u * half, s[0]);
-            tmem_ld32(t_s + 64u * half + 32u, s[1]);
-          }
-          if (!ok) break;
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            f32x2 sum0 = splat2(0.f), sum1 = splat2(0.f);
-            uint32_t w[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float a = __uint_as_float(s[q][2 * e]), b = __uint_as_float(s[q][2 * e + 1]);
-              if (e < 8) sum0 = add2(sum0, pack2(a, b)); else sum1 = add2(sum1, pack2(a, b));
-              w[e] = bits_of(__floats2half2_rn(a, b));
-            }
-            if (half == 0) tmem_ld32(t_s + 64u + 32u * q, s[q]);
-            tmem_st16(t_s + 32u * half + 16u * q, w);
-            float a, b;
-            unpack2(sum0, a, b);
-            z = fmaf(a + b, g[2 * q].z, z);
-            unpack2(sum1, a, b);
-            z = fmaf(a + b, g[2 * q + 1].z, z);
-          }
-          tmem_st_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&S.p_full[i][half]));
+          if (!__any_sync(0xffffffffu, top > m + kLag)) break;
+          // m rises: what has been summed so far is brought down
+          const float up = top > m + kLag ? top : m;
+          const float down = m == -CUDART_INF_F ? 0.f : ex2(m - up);
+          z *= down;
+          m = up;
+          base = m == -CUDART_INF_F ? 0.f : kLift - m;
+          if (u > 0 && !(ok = bring_down(S.pv_done[i][half ^ 1], (ph_pv >> (half ^ 1)) ^ 1u, abort, P.status, t_o, kSteps, down))) break;
         }
         if (!ok) break;
-        sees -= kKeys;
-        ph_pv ^= 1u;                                      // this step's completion comes next
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          f32x2 sum0 = splat2(0.f), sum1 = splat2(0.f);
+          uint32_t w[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float a = __uint_as_float(s[q][2 * e]), b = __uint_as_float(s[q][2 * e + 1]);
+            if (e < 8) sum0 = add2(sum0, pack2(a, b)); else sum1 = add2(sum1, pack2(a, b));
+            w[e] = bits_of(__floats2half2_rn(a, b));
+          }
+          tmem_st16(t_u + 16u * q, w);
+          float a, b;
+          unpack2(sum0, a, b);
+          z = fmaf(a + b, g[2 * q].z, z);
+          unpack2(sum1, a, b);
+          z = fmaf(a + b, g[2 * q + 1].z, z);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&S.p_full[i][half]));
+        sees -= kHalf;
+        ph_pv ^= 1u << half;                              // this step's product comes next
       }
       if (!ok) break;
       // the next item's queries come while the last product and the output run (the S MMAs have read this one's)
       more = see_item(it + 1);
       const volatile Item& y = S.item[(it + 1) & 1];
-      const bool q_next = more && y.end[i] > y.j0;
+      const bool q_next = more && y.ends[i] > 0;
       if (q_next) ask_q(y);
       if (n > 0) {
-        ok = __all_sync(0xffffffffu, wait_for(S.pv_done[i], ph_pv ^ 1u, abort, 112, P.status));
+        ok = __all_sync(0xffffffffu, wait_for(S.pv_done[i][(n - 1) & 1], (ph_pv >> ((n - 1) & 1)) ^ 1u, abort, 112, P.status));
         tc_fence_after();
       }
       if (q_next) give_q();
       if (!ok) break;
-      kg += uint32_t(max(max(x.end[0], x.end[1]) - x.j0, 0));
+      kg += uint32_t((max(x.ends[0], x.ends[1]) + 1) >> 1);
       const OutRow row = row_of(x);
 
       // ---- the row
