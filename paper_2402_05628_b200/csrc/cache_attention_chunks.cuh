@@ -13,7 +13,7 @@
 //
 // Items (request, row pair, head; the longest of a request first) are handed out by a counter; where there are fewer of them than SMs, each
 // is cut along the keys and joined by the part that finishes last, parts in order.
-// Roles: two groups of four softmax warps, four conversion warps, one warp that issues MMAs, one that fetches items.  Every wait is
+// Roles: two groups of four softmax warps, four conversion warps, a warp per tile that issues MMAs, one that fetches items.  Every wait is
 // bounded; when one runs out all roles leave, MMAs in flight are drained and tensor memory is freed.
 #pragma once
 #include <type_traits>
@@ -31,8 +31,8 @@ using namespace tc;
 constexpr int kTileRows = 128, kPair = 2 * kTileRows;
 constexpr int kKeys = 128, kHalf = 64;   // keys that are converted at a time, and that a tile takes at a time
 constexpr int kSoftWarps = 8, kConvWarps = 4;
-constexpr int kMmaWarp = kSoftWarps + kConvWarps, kItemWarp = kMmaWarp + 1;
-constexpr int kThreads = 512;             // (two warps of the last group have nothing to do)
+constexpr int kMmaWarp = kSoftWarps + kConvWarps, kItemWarp = kMmaWarp + 2;       // (an MMA warp per tile)
+constexpr int kThreads = 512;             // (the last warp has nothing to do)
 // Registers per thread, dealt out anew once the roles part: 256 x 176 + 128 x 80 + 128 x 80 = the 512 x 128 of the launch
 constexpr int kSoftRegs = 176, kConvRegs = 80, kOtherRegs = 80;
 constexpr float kLift = 7.f, kLag = 8.f;
@@ -60,7 +60,7 @@ struct Shared {
   Item item[2];
   int items, last[2];
   alignas(8) uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2][2], p_full[2][2], pv_done[2][2], o_empty[2], item_full[2],
-      item_empty[2], ask, done;
+      item_empty[2], ask, done[2];
   uint32_t tmem_base;
   volatile int abort;
 };
@@ -234,9 +234,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&S.k_full[i]), kConvWarps);
-      mbar_init(smem_u32(&S.k_empty[i]), 1);
+      mbar_init(smem_u32(&S.k_empty[i]), 2);
       mbar_init(smem_u32(&S.v_full[i]), kConvWarps);
-      mbar_init(smem_u32(&S.v_empty[i]), 1);
+      mbar_init(smem_u32(&S.v_empty[i]), 2);
       mbar_init(smem_u32(&S.q_full[i]), 4);
       mbar_init(smem_u32(&S.s_full[i][0]), 1);
       mbar_init(smem_u32(&S.s_full[i][1]), 1);
@@ -246,10 +246,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
       mbar_init(smem_u32(&S.pv_done[i][1]), 1);
       mbar_init(smem_u32(&S.o_empty[i]), 4);
       mbar_init(smem_u32(&S.item_full[i]), 1);
-      mbar_init(smem_u32(&S.item_empty[i]), kSoftWarps + kConvWarps + 1);
+      mbar_init(smem_u32(&S.item_empty[i]), kSoftWarps + kConvWarps + 2);
+      mbar_init(smem_u32(&S.done[i]), 1);
     }
-    mbar_init(smem_u32(&S.ask), 1);
-    mbar_init(smem_u32(&S.done), 1);
+    mbar_init(smem_u32(&S.ask), 2);
     S.abort = 0;
     if (smem_u32(smem_raw) & 1023u) {
       atomicCAS(P.status, 0, 100);
@@ -358,107 +358,100 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
         P.tickets[0] = 0;
         P.tickets[1] = 0;
       }
-    } else if (warp == kMmaWarp) {
-      // ---------------------------------------------------------------- MMAs
+    } else if (warp < kItemWarp) {
+      // ---------------------------------------------------------------- MMAs of tile i
+      // (The whole warp walks the loop and one lane issues; what an item is, is told as alike for all lanes, so that descriptors stay in
+      // uniform registers, from which MMAs take them: moved there one by one they took 150 cycles an MMA.  A warp for both tiles spent
+      // 800 cycles a step on its own instructions.)
+      const int i = warp - kMmaWarp;
       const bool issues = elect_one();
       // D = f32; S: A and B bf16, K-major, N = 64; P V: f16, A in tensor memory, B MN-major, N = d_h
       constexpr uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(kHalf >> 3) << 17) | (uint32_t(kTileRows >> 4) << 24);
       constexpr uint32_t idesc_o = (1u << 4) | (1u << 16) | (uint32_t(dh >> 3) << 17) | (uint32_t(kTileRows >> 4) << 24);
-      const uint64_t dq0 = smem_desc_sw128(smem_u32(S.q[0])), dk0 = smem_desc_sw128(smem_u32(S.k[0])),
+      constexpr uint32_t kTileUnits = Sh::kTile >> 4, kHalfUnits = kHalf * 128 / 16;
+      const uint64_t dq = smem_desc_sw128(smem_u32(S.q[0])) + uint64_t(uint32_t(i) * kTileUnits), dk0 = smem_desc_sw128(smem_u32(S.k[0])),
                      dv0 = smem_desc_sw128(smem_u32(S.v[0]), 128 * 128);
-      uint32_t g = 0;                                     // steps of 128 keys taken before this item
-      uint32_t ph_q = 0, ph_p = 0, ph_o = 0;              // a bit per tile (ph_p: per tile and half)
+      const uint32_t t_s = tmem + uint32_t(i * 128), t_o = tmem + 256u + uint32_t(i * 128);
+      uint32_t g = 0, tiles = 0;                          // steps of 128 keys and items with rows of this tile, before this item
+      uint32_t ph_p = 0;                                  // a bit per half
       bool ok = true;
+      auto await = [&](uint64_t& bar, uint32_t phase, int code) {
+        ok = ok && wait_for(bar, phase, abort, code, P.status);
+        ok = __all_sync(0xffffffffu, ok);
+        return ok;
+      };
+      // S of a half of the keys of slot `k` into the half of the tile's columns whose weights the product before last has taken
+      auto issue_s = [&](uint32_t k, int half) {
+        tc_fence_after();
+        if (issues) {
+          const uint64_t b = dk0 + uint64_t(k * kTileUnits + uint32_t(half) * kHalfUnits);
+#pragma unroll
+          for (int s = 0; s < kSteps; ++s) {
+            const uint32_t off = uint32_t(s >> 2) * (128 * 128 / 16) + uint32_t(s & 3) * 2;
+            umma_f16(t_s + uint32_t(half * 64), dq + off, b + off, idesc_s, s != 0 ? 1u : 0u);
+          }
+          umma_commit(smem_u32(&S.s_full[i][half]));
+        }
+        __syncwarp();
+      };
+      auto issue_pv = [&](uint32_t v, int half, bool first) {
+        ph_p ^= 1u << half;
+        tc_fence_after();
+        if (issues) {
+          const uint64_t b = dv0 + uint64_t(v * kTileUnits + uint32_t(half) * kHalfUnits);
+#pragma unroll
+          for (int s = 0; s < kHalf / 16; ++s)
+            umma_f16_ts(t_o, t_s + uint32_t(half * 64 + 8 * s), b + uint64_t(16 * 128 / 16 * s), idesc_o, !first || s != 0 ? 1u : 0u);
+          umma_commit(smem_u32(&S.pv_done[i][half]));
+        }
+        __syncwarp();
+      };
+      auto release = [&](uint64_t& bar) {                 // once the MMAs issued so far are done
+        if (issues) umma_commit(smem_u32(&bar));
+        __syncwarp();
+      };
       Item x;
       for (int it = 0; ok && next_item(it, x); ++it) {
-        // (steps of 64 keys; told as alike for all lanes: descriptors then stay in uniform registers, from which MMAs take them.  Moved there
-        // one by one they took 150 cycles an MMA.)
-        const int ends[2] = {__shfl_sync(0xffffffffu, x.ends[0], 0), __shfl_sync(0xffffffffu, x.ends[1], 0)};
-        const int n = max(ends[0], ends[1]);
-        if (n <= 6 && lane == 0) mbar_arrive(smem_u32(&S.ask));
+        const int end = __shfl_sync(0xffffffffu, x.ends[i], 0), other = __shfl_sync(0xffffffffu, x.ends[i ^ 1], 0);    // steps of 64 keys
+        const int n = (max(end, other) + 1) >> 1;         // steps of 128
+        if (n <= 3 && lane == 0) mbar_arrive(smem_u32(&S.ask));
         if (n <= 0) continue;
-        int k_there = -1, v_there = -1;                   // steps of 128 whose tiles have been waited for
-        auto keys = [&](int u) {
-          if ((u >> 1) > k_there) {
-            const uint32_t at = g + uint32_t(u >> 1);
-            ok = __all_sync(0xffffffffu, wait_for(S.k_full[at & 1], at >> 1, abort, 103, P.status));
-            k_there = u >> 1;
-            tc_fence_after();
-          }
-          return ok;
-        };
-        // S of step u into the half of the tile's columns whose weights the product of step u - 2 has taken
-        auto issue_s = [&](int i, int u) {
-          if (issues) {
-            const uint64_t a = dq0 + uint64_t(i * (Sh::kTile >> 4));
-            const uint64_t b = dk0 + uint64_t(((g + uint32_t(u >> 1)) & 1) * (Sh::kTile >> 4)) + uint64_t((u & 1) * (kHalf * 128 / 16));
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-              const uint32_t off = uint32_t(s >> 2) * (128 * 128 / 16) + uint32_t(s & 3) * 2;
-              umma_f16(tmem + uint32_t(i * 128 + (u & 1) * 64), a + off, b + off, idesc_s, s != 0 ? 1u : 0u);
-            }
-            umma_commit(smem_u32(&S.s_full[i][u & 1]));
-          }
-          __syncwarp();
-        };
-        auto keys_read = [&](int u) {                     // both tiles' S of step u are issued
-          if (issues && ((u & 1) || u + 1 == n)) umma_commit(smem_u32(&S.k_empty[(g + uint32_t(u >> 1)) & 1]));
-          __syncwarp();
-        };
-#pragma unroll 1
-        for (int u = 0; u < min(n, 2) && ok; ++u) {
-          if (!keys(u)) break;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            if (u >= ends[i]) continue;
-            if (u == 0) {
-              if (!(ok = __all_sync(0xffffffffu, wait_for(S.q_full[i], ph_q >> i, abort, 104, P.status)))) break;
-              ph_q ^= 1u << i;
-              tc_fence_after();
-            }
-            issue_s(i, u);
-          }
-          if (ok) keys_read(u);
+        if (!await(S.k_full[g & 1], g >> 1, 103)) break;
+        if (end > 0) {
+          if (!await(S.q_full[i], tiles, 104)) break;
+          issue_s(g & 1, 0);
+          if (end > 1) issue_s(g & 1, 1);
         }
+        release(S.k_empty[g & 1]);
 #pragma unroll 1
-        for (int u = 0; u < n && ok; ++u) {
-          if (u + 6 == n && lane == 0) mbar_arrive(smem_u32(&S.ask));
-          const uint32_t at = g + uint32_t(u >> 1);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            if (u >= ends[i]) continue;
-            if ((u >> 1) > v_there) { ok = wait_for(S.v_full[at & 1], at >> 1, abort, 106, P.status); v_there = u >> 1; }
-            if (ok && u == 0) { ok = wait_for(S.o_empty[i], (ph_o >> i) ^ 1u, abort, 107, P.status); ph_o ^= 1u << i; }
-            const int slot = 2 * i + (u & 1);
-            ok = ok && wait_for(S.p_full[i][u & 1], ph_p >> slot, abort, 105, P.status);
-            if (!(ok = __all_sync(0xffffffffu, ok))) break;
-            ph_p ^= 1u << slot;
-            tc_fence_after();
-            if (issues) {
-              const uint64_t b = dv0 + uint64_t((at & 1) * (Sh::kTile >> 4)) + uint64_t((u & 1) * (kHalf * 128 / 16));
-#pragma unroll
-              for (int s = 0; s < kHalf / 16; ++s)
-                umma_f16_ts(tmem + 256u + uint32_t(i * 128), tmem + uint32_t(i * 128 + (u & 1) * 64 + 8 * s), b + uint64_t(16 * 128 / 16 * s), idesc_o,
-                            u != 0 || s != 0 ? 1u : 0u);
-              umma_commit(smem_u32(&S.pv_done[i][u & 1]));
-            }
-            __syncwarp();
-            if (u + 2 < ends[i]) {
-              if (!keys(u + 2)) break;
-              issue_s(i, u + 2);
-            }
+        for (int j = 0; j < n; ++j) {
+          if (j + 3 == n && lane == 0) mbar_arrive(smem_u32(&S.ask));
+          const uint32_t at = g + uint32_t(j), next = at + 1;
+          const int left = end - 2 * j;                   // of the tile's steps
+          if (!await(S.v_full[at & 1], at >> 1, 106)) break;
+          if (left > 0) {
+            if (j == 0 && !await(S.o_empty[i], tiles ^ 1u, 107)) break;
+            if (!await(S.p_full[i][0], ph_p, 105)) break;
+            issue_pv(at & 1, 0, j == 0);
           }
-          if (!ok) break;
-          if (u + 2 < n) keys_read(u + 2);
-          if (issues && ((u & 1) || u + 1 == n)) umma_commit(smem_u32(&S.v_empty[at & 1]));
-          __syncwarp();
+          if (j + 1 < n && !await(S.k_full[next & 1], next >> 1, 103)) break;
+          if (left > 2) issue_s(next & 1, 0);
+          if (left > 1) {
+            if (!await(S.p_full[i][1], ph_p >> 1, 105)) break;
+            issue_pv(at & 1, 1, false);
+          }
+          release(S.v_empty[at & 1]);
+          if (left > 3) issue_s(next & 1, 1);
+          if (j + 1 < n) release(S.k_empty[next & 1]);
         }
-        g += uint32_t((n + 1) >> 1);
+        if (!ok) break;
+        g += uint32_t(n);
+        tiles += end > 0 ? 1u : 0u;
       }
-      if (issues) umma_commit(smem_u32(&S.done));
+      if (issues) umma_commit(smem_u32(&S.done[i]));
       __syncwarp();
-      mbar_drain(smem_u32(&S.done), 0);
-  }
+      mbar_drain(smem_u32(&S.done[i]), 0);
+    }
   } else if (warp >= kSoftWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kConvRegs));
     // ---------------------------------------------------------------- codes to f16 tiles
