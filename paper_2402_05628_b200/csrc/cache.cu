@@ -2,6 +2,7 @@
 #include <cuda_bf16.h>
 
 #include "cache.cuh"
+#include "f32x2.cuh"
 #include "kernels.h"
 
 namespace repq {
@@ -144,27 +145,54 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const __grid_c
   }
 }
 
-// ---- write.  Bytes are all there is to it (a row read, a row of codes written), but a block's scale needs all of the rows that it gets: a warp takes one
-// head's K or V rows of one block ("run"), 16 of them at a time in registers where they fit.  CTAs take windows of consecutive tokens, so that the
-// tokens that do not start a run cost a vote and no launch.
-constexpr int kWriteWarps = 8;
+// ---- write.  Bytes are all there is to it (a row read, a row of codes written), but a block's scale needs all of the rows that it gets ("run": rows
+// of consecutive slots in one block).  A CTA takes a window of tokens and K or V of one head; the window's runs are found by a vote.  A run that
+// fits a warp's registers (16 rows of 128 channels) is a warp's; a longer one is shared by the CTA's warps, which join their
+// maxima in shared memory.  Either way every row is read once, all its loads in flight together (a run per warp whatever its length, read
+// twice where it did not fit: 75 us for 2400 tokens of 32 heads of 128 channels in blocks of 64; floor 9).
+constexpr int kHeld = 8;                          // pieces of eight elements that a thread holds
+constexpr int kMostWindow = 128;
 
 struct WriteParams {
   repq_cache c;
   const void* x[2];
   int64_t st[2], sh[2];
   const int32_t* slots;
-  int tokens, shift, window, tasks;               // tasks: kv_heads * 2
+  int tokens, shift, window;
+  int pieces, by_pieces;                          // pieces of a row; n / pieces = n * by_pieces >> 16 for n < 2048
 };
 
-__device__ __forceinline__ float magnitude(float a) { return fminf(fabsf(a), 3.402823466e38f); }   // (fminf drops a NaN ...)
-
-// round(x / s) to a code, as the IEEE quotient rounds: x * (1 / s) is within 2^-15 of it where codes are, so only quotients near a tie are divided
-__device__ __forceinline__ uint32_t code_of(float x, float s, float inv) {
-  float t = x * inv, q = rintf(t);
-  if (fabsf(fabsf(t - q) - 0.5f) < 1e-4f) q = rintf(__fdiv_rn(x, s));
-  q = fminf(fmaxf(q, -127.f), 127.f);
+// round(x / s) to a code, as the IEEE quotient rounds, a NaN to 128 ...
+__device__ __forceinline__ uint32_t exact_code(float x, float s) {
+  const float q = fminf(fmaxf(rintf(__fdiv_rn(x, s)), -127.f), 127.f);
   return x == x ? uint32_t(int(q) + 128) : 128u;
+}
+static __device__ __noinline__ uint2 exact_codes(float4 a, float4 b, float s) {
+  return make_uint2(exact_code(a.x, s) | exact_code(a.y, s) << 8 | exact_code(a.z, s) << 16 | exact_code(a.w, s) << 24,
+                    exact_code(b.x, s) | exact_code(b.y, s) << 8 | exact_code(b.z, s) << 16 | exact_code(b.w, s) << 24);
+}
+// ... of eight elements: x * (1 / s) is within 2^-15 of the quotient where codes are, so only pieces with a value near a tie (or an infinity
+// or NaN) are divided, one in 150; all other roundings are those of the float adder (1.5 * 2^23 + 128, whose low byte is the code).
+// (A division of every element inlined: 38 instructions an element, 49 us for what takes 9 at the memory's rate.)
+__device__ __forceinline__ uint2 codes_of(const float (&f)[8], float s, float inv) {
+  constexpr float kMagic = 12582912.f + 128.f;
+  const f32x2 inv2 = splat2(inv), up = splat2(kMagic), down = splat2(-kMagic);
+  uint32_t u[8];
+  bool plain = true;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const f32x2 t = mul2(pack2(f[2 * k], f[2 * k + 1]), inv2), q = add2(t, up), back = add2(q, down);
+    float t0, t1, q0, q1, b0, b1;
+    unpack2(t, t0, t1);
+    unpack2(q, q0, q1);
+    unpack2(back, b0, b1);
+    plain = plain && fabsf(t0 - b0) < 0.4999f && fabsf(t1 - b1) < 0.4999f;
+    u[2 * k] = __float_as_uint(q0);
+    u[2 * k + 1] = __float_as_uint(q1);
+  }
+  if (!plain) return exact_codes(make_float4(f[0], f[1], f[2], f[3]), make_float4(f[4], f[5], f[6], f[7]), s);
+  return make_uint2(__byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410),
+                    __byte_perm(__byte_perm(u[4], u[5], 0x0040), __byte_perm(u[6], u[7], 0x0040), 0x5410));
 }
 
 template <typename T> struct Piece;               // eight elements
@@ -177,6 +205,12 @@ template <> struct Piece<__nv_bfloat16> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
   }
+  // largest magnitude (NaN left out)
+  __device__ __forceinline__ float top() const {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&r);
+    const __nv_bfloat162 m = __hmax2(__hmax2(__habs2(h[0]), __habs2(h[1])), __hmax2(__habs2(h[2]), __habs2(h[3])));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
 };
 template <> struct Piece<float> {
   float4 a, b;
@@ -188,112 +222,116 @@ template <> struct Piece<float> {
   __device__ __forceinline__ void get(float (&f)[8]) const {
     f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
   }
+  __device__ __forceinline__ float top() const {
+    return fmaxf(fmaxf(fmaxf(fabsf(a.x), fabsf(a.y)), fmaxf(fabsf(a.z), fabsf(a.w))), fmaxf(fmaxf(fabsf(b.x), fabsf(b.y)), fmaxf(fabsf(b.z), fabsf(b.w))));
+  }
 };
 
-// kHeld pieces of eight elements per lane stay in registers between the maximum and the codes; a run of more rows reads them again.
-template <typename T, int kHeld>
-__global__ void __launch_bounds__(32 * kWriteWarps) cache_write_kernel(const __grid_constant__ WriteParams P) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int task = blockIdx.y * kWriteWarps + warp;
-  grid_dependency_wait();
-  grid_dependency_trigger();
-  if (task >= P.tasks) return;
-  const int head = task >> 1, kv = task & 1;
-  const int bs = 1 << P.shift, pieces = P.c.d_h >> 3;
+// A run's rows, by `kThreads` threads of which this is number `t`: a warp, or the whole CTA (`tops`: a word per warp in shared memory).
+template <typename T, int kThreads>
+__device__ __forceinline__ void write_run(const WriteParams& P, int head, int kv, int t0, int slot0, int rows, int t, uint32_t* tops) {
+  const int lane = t & 31, bs = 1 << P.shift, off = slot0 & (bs - 1), page = slot0 >> P.shift;
+  const int64_t tile = int64_t(page) * P.c.kv_heads + head;
+  const int64_t st = kv ? P.st[1] : P.st[0];
+  const T* x = static_cast<const T*>(kv ? P.x[1] : P.x[0]) + head * (kv ? P.sh[1] : P.sh[0]) + t0 * st;
+  uint8_t* codes = (kv ? P.c.v_codes : P.c.k_codes) + (tile << P.shift) * P.c.d_h;
+  float* scale = (kv ? P.c.v_scale : P.c.k_scale) + tile;
+  const int n = rows * P.pieces;
+  Piece<T> held[kHeld];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int e = t + kThreads * i;
+    if (e < n) { const int r = e * P.by_pieces >> 16; held[i].load(x + r * st + 8 * (e - r * P.pieces)); }
+    else held[i].clear();
+  }
+  const float before = off ? *scale : 0.f;
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) top = fmaxf(top, held[i].top());
+  top = fminf(top, 3.402823466e38f);
+  // (magnitudes order as their bits do)
+  uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
+  if (kThreads > 32) {
+    if (lane == 0) tops[t >> 5] = bits;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) bits = max(bits, tops[w]);
+  }
+  const float after = fmaxf(before, fmaxf(__fmul_rn(__uint_as_float(bits), 1.0f / 127.0f), 0x1p-60f));
+  if (after > before) {
+    if (off) {                                     // the block's earlier rows move to the wider scale
+      const float ratio = __fdiv_rn(before, after);
+      uint32_t* w = reinterpret_cast<uint32_t*>(codes);
+#pragma unroll 1
+      for (int e = t; e < (off * P.c.d_h) >> 2; e += kThreads) {
+        const uint32_t u = w[e];
+        uint32_t o = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float c = fminf(fmaxf(rintf(__fmul_rn(float(int((u >> (8 * k)) & 255u) - 128), ratio)), -127.f), 127.f);
+          o |= uint32_t(int(c) + 128) << (8 * k);
+        }
+        w[e] = o;
+      }
+    }
+    if (kThreads > 32) __syncthreads();            // (every warp has read the scale)
+    if (t == 0) *scale = after;
+  }
+  const float inv = __fdiv_rn(1.0f, after);
+  uint2* to = reinterpret_cast<uint2*>(codes + off * P.c.d_h);
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int e = t + kThreads * i;
+    if (e >= n) break;
+    float f[8];
+    held[i].get(f);
+    to[e] = codes_of(f, after, inv);               // (rows of codes are dense: piece e of the run is 8 e bytes in)
+  }
+}
+
+template <typename T, int kThreads>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 768 / kThreads : 512 / kThreads) cache_write_kernel(const __grid_constant__ WriteParams P) {
+  constexpr int kWarps = kThreads / 32, kFits = 32 * kHeld;             // pieces of a warp
+  __shared__ uint32_t tops[2][kWarps];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int head = blockIdx.y, kv = blockIdx.z, bs = 1 << P.shift;
   const int t_end = min((int(blockIdx.x) + 1) * P.window, P.tokens);
   const int64_t slots = int64_t(P.c.num_blocks) << P.shift;
-  const T* base = static_cast<const T*>(kv ? P.x[1] : P.x[0]) + head * (kv ? P.sh[1] : P.sh[0]);
-  const int64_t st = kv ? P.st[1] : P.st[0];
-  uint8_t* codes_base = kv ? P.c.v_codes : P.c.k_codes;
-  float* scale_base = kv ? P.c.v_scale : P.c.k_scale;
+  grid_dependency_wait();
+  grid_dependency_trigger();
+  // (every warp finds the runs for itself: no barriers)
+  int nth = 0, shared = 0;
+#pragma unroll 1
   for (int w0 = int(blockIdx.x) * P.window; w0 < t_end; w0 += 32) {
     const int t = w0 + lane;
-    bool starts = false;
-    if (t < t_end) {
-      const int s = __ldg(P.slots + t);
-      starts = s >= 0 && s < slots && (t == 0 || (s & (bs - 1)) == 0 || __ldg(P.slots + t - 1) != s - 1);
-    }
-    uint32_t todo = __ballot_sync(0xffffffffu, starts);
+    const int s = t < P.tokens ? __ldg(P.slots + t) : -1, edge = lane == 0 && t > 0 && t < P.tokens ? __ldg(P.slots + t - 1) : -2;
+    int ahead = __shfl_up_sync(0xffffffffu, s, 1);
+    if (lane == 0) ahead = edge;
+    const bool there = s >= 0 && s < slots, starts = there && ((s & (bs - 1)) == 0 || ahead != s - 1);
+    uint32_t todo = __ballot_sync(0xffffffffu, starts && t < t_end);
+    const uint32_t breaks = __ballot_sync(0xffffffffu, starts || !there);
+#pragma unroll 1
     while (todo) {
-      const int t0 = w0 + __ffs(todo) - 1;
+      const int l0 = __ffs(todo) - 1, t0 = w0 + l0;
       todo &= todo - 1;
-      const int slot0 = __ldg(P.slots + t0), off = slot0 & (bs - 1), page = slot0 >> P.shift;
-      int rows = 0;                                // of the run: consecutive slots up to the block's end
-      for (; rows < bs - off; rows += 32) {
-        const int i = rows + lane;
-        const bool in = i < bs - off && t0 + i < P.tokens && __ldg(P.slots + t0 + i) == slot0 + i;
-        const uint32_t m = ~__ballot_sync(0xffffffffu, in);
-        if (m) { rows += __ffs(m) - 1; break; }
-      }
-      rows = min(rows, bs - off);
-      const int64_t tile = int64_t(page) * P.c.kv_heads + head;
-      uint8_t* codes = codes_base + (tile << P.shift) * P.c.d_h;
-      const float before = off ? scale_base[tile] : 0.f;
-      const T* x = base + t0 * st;
-      const int n = rows * pieces;                 // pieces of the run
-      float top = 0.f;
-      Piece<T> held[kHeld];
-#pragma unroll
-      for (int i = 0; i < kHeld; ++i) {
-        const int e = lane + 32 * i;
-        if (e < n) { const int r = e / pieces; held[i].load(x + r * st + 8 * (e - r * pieces)); }
-        else held[i].clear();
-      }
-      float f[8];
-#pragma unroll
-      for (int i = 0; i < kHeld; ++i) {
-        held[i].get(f);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) top = fmaxf(top, f[k] == f[k] ? magnitude(f[k]) : 0.f);
-      }
-      for (int e = lane + 32 * kHeld; e < n; e += 32) {
-        Piece<T> p;
-        const int r = e / pieces;
-        p.load(x + r * st + 8 * (e - r * pieces));
-        p.get(f);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) top = fmaxf(top, f[k] == f[k] ? magnitude(f[k]) : 0.f);
-      }
-      // (magnitudes order as their bits do)
-      top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
-      const float after = fmaxf(before, fmaxf(__fmul_rn(top, 1.0f / 127.0f), 0x1p-60f));
-      if (after > before) {
-        if (off) {                                 // the block's earlier rows move to the wider scale
-          const float ratio = __fdiv_rn(before, after);
-          uint32_t* w = reinterpret_cast<uint32_t*>(codes);
-          for (int e = lane; e < (off * P.c.d_h) >> 2; e += 32) {
-            const uint32_t u = w[e];
-            uint32_t o = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float c = fminf(fmaxf(rintf(__fmul_rn(float(int((u >> (8 * k)) & 255u) - 128), ratio)), -127.f), 127.f);
-              o |= uint32_t(int(c) + 128) << (8 * k);
-            }
-            w[e] = o;
-          }
+      const int slot0 = __shfl_sync(0xffffffffu, s, l0);
+      const uint32_t after = l0 == 31 ? 0u : breaks >> (l0 + 1);
+      int rows = after ? __ffs(after) : 32 - l0;   // up to what breaks the run, or to the end of these tokens
+      if (!after) {
+        const int most = min(bs - (slot0 & (bs - 1)), P.tokens - t0);
+#pragma unroll 1
+        for (; rows < most; rows += 32) {
+          const bool in = rows + lane < most && __ldg(P.slots + t0 + rows + lane) == slot0 + rows + lane;
+          const uint32_t m = ~__ballot_sync(0xffffffffu, in);
+          if (m) { rows += __ffs(m) - 1; break; }
         }
-        if (lane == 0) scale_base[tile] = after;
+        rows = min(rows, most);
       }
-      const float inv = __fdiv_rn(1.0f, after);
-      uint2* to = reinterpret_cast<uint2*>(codes + off * P.c.d_h);
-      auto put = [&](const Piece<T>& p, int e) {
-        p.get(f);
-        uint32_t c[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) c[k] = code_of(f[k], after, inv);
-        uint2 o;
-        o.x = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
-        o.y = __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410);
-        to[e] = o;                                 // (rows of codes are dense: piece e of the run is 8 e bytes in)
-      };
-#pragma unroll
-      for (int i = 0; i < kHeld; ++i)
-        if (lane + 32 * i < n) put(held[i], lane + 32 * i);
-      for (int e = lane + 32 * kHeld; e < n; e += 32) {
-        Piece<T> p;
-        const int r = e / pieces;
-        p.load(x + r * st + 8 * (e - r * pieces));
-        put(p, e);
+      if (rows * P.pieces <= kFits) {
+        if (nth++ % kWarps == warp) write_run<T, 32>(P, head, kv, t0, slot0, rows, lane, nullptr);
+      } else {
+        // (two sets of words in turn: a warp may be a run ahead of those that still read)
+        write_run<T, kThreads>(P, head, kv, t0, slot0, rows, tid, tops[shared++ & 1]);
       }
     }
   }
@@ -301,9 +339,10 @@ __global__ void __launch_bounds__(32 * kWriteWarps) cache_write_kernel(const __g
 
 template <typename T>
 repq_status launch_write(const WriteParams& P, cudaStream_t st) {
-  const dim3 grid((P.tokens + P.window - 1) / P.window, (P.tasks + kWriteWarps - 1) / kWriteWarps);
-  if (P.window == 1) REPQ_CUDA(launch_chained(cache_write_kernel<T, 1>, grid, dim3(32 * kWriteWarps), 0, st, P));
-  else REPQ_CUDA(launch_chained(cache_write_kernel<T, 8>, grid, dim3(32 * kWriteWarps), 0, st, P));
+  const dim3 grid((P.tokens + P.window - 1) / P.window, P.c.kv_heads, 2);
+  // four warps hold 64 rows of 128 channels
+  if (P.shift <= 6) REPQ_CUDA(launch_chained(cache_write_kernel<T, 128>, grid, dim3(128), 0, st, P));
+  else REPQ_CUDA(launch_chained(cache_write_kernel<T, 256>, grid, dim3(256), 0, st, P));
   note_launch();
   return REPQ_OK;
 }
@@ -353,12 +392,13 @@ extern "C" repq_status repq_cache_write(const repq_cache_write_desc* d, void* st
   P.slots = d->slot_map;
   P.tokens = d->tokens;
   P.shift = cache::log2_block(d->cache.block_size);
-  P.tasks = 2 * d->cache.kv_heads;
-  // a window per CTA such that there are some 32 warps per SM; one token where there are few
-  const int64_t per = int64_t(d->tokens) * P.tasks / (int64_t(sm_count()) * 32);
-  P.window = 1;
-  while (P.window < per && P.window < 128) P.window *= 2;
-  REPQ_REQUIRE((P.tasks + 7) / 8 <= 65535, REPQ_UNSUPPORTED, "repq_cache_write: too many heads");
+  P.pieces = d->cache.d_h / 8;
+  P.by_pieces = (65536 + P.pieces - 1) / P.pieces;
+  // windows such that there are some sixteen CTAs per SM; four tokens where there are few (a warp each)
+  const int64_t per = int64_t(d->tokens) * d->cache.kv_heads / (int64_t(sm_count()) * 8);
+  P.window = 4;
+  while (P.window < per && P.window < cache::kMostWindow) P.window *= 2;
+  REPQ_REQUIRE(d->cache.kv_heads <= 65535, REPQ_UNSUPPORTED, "repq_cache_write: too many heads");
   return d->dtype == REPQ_F32 ? cache::launch_write<float>(P, static_cast<cudaStream_t>(stream))
                               : cache::launch_write<__nv_bfloat16>(P, static_cast<cudaStream_t>(stream));
 }

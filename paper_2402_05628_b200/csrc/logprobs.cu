@@ -13,6 +13,7 @@ constexpr int kMostTop = 32;
 constexpr int kCand = 256;                        // candidates of a CTA
 constexpr int kMostSplit = 8;                     // CTAs of a row (a cluster)
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kFloor = -1.7e38f;
 
 struct Params {
   const void* x;
@@ -43,12 +44,14 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// What a stretch of a row says: m = max x (NaN left out), z = sum 2^(c (x - m)), w = sum 2^(c (x - m)) c (x - m), c = log2 e.
+// What a stretch of a row says: z = sum e^(x - m), w = sum e^(x - m) (x - m), for an m that is at most kLag below max x
+// (NaN left out): sums in float32 have room for it, and m moves rarely.
+constexpr float kLag = 20.f;
 struct Stats { float m, z, w; };
 __device__ __forceinline__ void move_to(Stats& a, float m) {      // m >= a.m
   if (a.m == m) return;
-  const float d = fmaxf((a.m - m) * kLog2e, -1e30f);              // (-inf where nothing has been seen: z = w = 0)
-  const float f = ex2(d);
+  const float d = fmaxf(a.m - m, -1e30f);                         // (-inf where nothing has been seen: z = w = 0)
+  const float f = ex2(d * kLog2e);
   a.w = f * fmaf(a.z, d, a.w);
   a.z *= f;
   a.m = m;
@@ -67,6 +70,27 @@ template <> struct Vec<float> {
     f[0] = __uint_as_float(r.x); f[1] = __uint_as_float(r.y); f[2] = __uint_as_float(r.z); f[3] = __uint_as_float(r.w);
   }
   __device__ __forceinline__ static float one(const void* p, int64_t i) { return __ldg(static_cast<const float*>(p) + i); }
+  // largest element (NaN left out)
+  __device__ __forceinline__ static float top(const uint4& r) {
+    float f[4];
+    get(r, f);
+    return fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3]));
+  }
+  // -inf (and all below -1.7e38) as -1.7e38; a NaN stays
+  __device__ __forceinline__ static uint4 floored(const uint4& r) {
+    float f[4];
+    get(r, f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(f[i]) : "f"(kFloor));
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  }
+  // elements above x, in a word whose two halves add up
+  __device__ __forceinline__ static uint32_t above(const uint4& r, float x) {
+    float f[4];
+    get(r, f);
+    return uint32_t(f[0] > x) + uint32_t(f[1] > x) + uint32_t(f[2] > x) + uint32_t(f[3] > x);
+  }
+  static constexpr int kLow = 0;                   // bits below the type's last
 };
 template <> struct Vec<__nv_bfloat16> {
   static constexpr int kN = 8;
@@ -76,16 +100,76 @@ template <> struct Vec<__nv_bfloat16> {
     for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
   }
   __device__ __forceinline__ static float one(const void* p, int64_t i) { return __bfloat162float(__ldg(static_cast<const __nv_bfloat16*>(p) + i)); }
+  __device__ __forceinline__ static __nv_bfloat162 pair(const uint32_t& w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
+  __device__ __forceinline__ static float top(const uint4& r) {
+    const __nv_bfloat162 a = __hmax2(__hmax2(pair(r.x), pair(r.y)), __hmax2(pair(r.z), pair(r.w)));
+    return fmaxf(__low2float(a), __high2float(a));
+  }
+  __device__ __forceinline__ static uint4 floored(const uint4& r) {
+    const __nv_bfloat162 k = __float2bfloat162_rn(kFloor);
+    const __nv_bfloat162 a = __hmax2_nan(pair(r.x), k), b = __hmax2_nan(pair(r.y), k), c = __hmax2_nan(pair(r.z), k), d = __hmax2_nan(pair(r.w), k);
+    return make_uint4(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b), *reinterpret_cast<const uint32_t*>(&c),
+                      *reinterpret_cast<const uint32_t*>(&d));
+  }
+  __device__ __forceinline__ static uint32_t above(const uint4& r, float x) {   // (x is a bf16 number)
+    const __nv_bfloat162 x2 = __float2bfloat162_rn(x);
+    constexpr uint32_t k1 = 0x00010001u;
+    return (__hgt2_mask(pair(r.x), x2) & k1) + (__hgt2_mask(pair(r.y), x2) & k1) + (__hgt2_mask(pair(r.z), x2) & k1) + (__hgt2_mask(pair(r.w), x2) & k1);
+  }
+  static constexpr int kLow = 16;
 };
 
+// The next number of the type below x (x neither -inf nor NaN): what is above it is x or more.
 template <typename T>
+__device__ __forceinline__ float below(float x) {
+  const uint32_t u = __float_as_uint(x), step = 1u << Vec<T>::kLow;
+  if ((u & 0x7fffffffu) == 0u) return __uint_as_float(0x80000000u | step);
+  return __uint_as_float((u & 0x80000000u) ? u + step : u - step);
+}
+
+// kWhole: rows are 16-byte aligned and whole vectors; otherwise element by element where they are not, -inf past the stretch's end.
+template <typename T, bool kWhole>
 __device__ __forceinline__ uint4 load_vec(const Params& P, const T* row, int e, int end) {
   constexpr int kN = Vec<T>::kN;
-  if (P.vec && e + kN <= end) return __ldg(reinterpret_cast<const uint4*>(row + e));
-  union { T t[kN]; uint4 r; } u;
+  if constexpr (kWhole) {
+    return __ldg(reinterpret_cast<const uint4*>(row + e));
+  } else {
+    if (P.vec && e + kN <= end) return __ldg(reinterpret_cast<const uint4*>(row + e));
+    union { T t[kN]; uint4 r; } u;
 #pragma unroll
-  for (int i = 0; i < kN; ++i) u.t[i] = e + i < end ? row[e + i] : T(-CUDART_INF_F);
-  return u.r;
+    for (int i = 0; i < kN; ++i) u.t[i] = e + i < end ? row[e + i] : T(-CUDART_INF_F);
+    return u.r;
+  }
+}
+
+// The sums' share of a vector where nothing above -1e38 has been seen yet.
+template <typename T>
+static __device__ __noinline__ float2 careful_sums(uint4 v, float base) {
+  constexpr int kN = Vec<T>::kN;
+  float f[kN], z = 0.f, w = 0.f;
+  Vec<T>::get(v, f);
+#pragma unroll 1
+  for (int i = 0; i < kN; ++i) {
+    const float d = f[i] - base, p = ex2(d * kLog2e);
+    z += p;
+    w = fmaf(p, fmaxf(d, -1e30f), w);              // (0 * -inf)
+  }
+  return make_float2(z, w);
+}
+
+// A vector's elements from `least` on up, as candidates.
+template <typename T>
+static __device__ __noinline__ void pick(uint4 v, int at, int end, float least, int* n_cand, uint64_t* cand) {
+  constexpr int kN = Vec<T>::kN;
+  float f[kN];
+  if (Vec<T>::top(v) < least) return;
+  Vec<T>::get(v, f);
+#pragma unroll
+  for (int i = 0; i < kN; ++i)
+    if (f[i] >= least && at + i < end) {
+      const int n = atomicAdd(n_cand, 1);
+      if (n < kCand) cand[n] = key_of(f[i], at + i);
+    }
 }
 
 __device__ __forceinline__ uint32_t cluster_addr(const void* p, int rank) {
@@ -107,11 +191,12 @@ __device__ __forceinline__ void put_remote64(uint32_t addr, uint64_t v) {
 // The first pass has the maximum, the sums, the number of tokens ahead of the given one, and every thread's largest element.  The K-th
 // largest of 64 disjoint groups' largest elements bounds the K-th largest element from below, so a second look at the stretch (from
 // cache) picks the few elements above that bound, which are then sorted by counting.
-template <typename T, int kThreads, int kSplit>
+template <typename T, int kThreads, int kSplit, bool kWhole>
 __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const __grid_constant__ Params P) {
   constexpr int kN = Vec<T>::kN, kWarps = kThreads / 32, kFly = 4;
   __shared__ Stats warp_stats[kWarps];
   __shared__ int warp_ahead[kWarps];
+  __shared__ float warp_most[kWarps];
   __shared__ uint64_t cand[kCand];
   __shared__ float group_top[64];
   __shared__ int n_cand;
@@ -131,54 +216,102 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const __grid_c
   const int token = P.tokens ? __ldg(P.tokens + r) : -1;
   const bool given = token >= 0 && token < P.vocab;
   const float xt = given ? Vec<T>::one(row, token) : 0.f;
+  const bool strange = given && !(xt > -CUDART_INF_F);                      // -inf or NaN: counted on their own
+  const float xb = strange ? xt : below<T>(xt);
 
   Stats s = {-CUDART_INF_F, 0.f, 0.f};
   int ahead = 0;
+  uint32_t ahead2 = 0u;
+  float best = -CUDART_INF_F;                      // the thread's largest element, in the vector that begins at best_e
+  int best_e = begin;
+  f32x2 z2 = splat2(0.f), w2 = splat2(0.f);        // sums of the pairs' halves since m last moved
+  auto settle = [&]() {
+    float a, b;
+    unpack2(z2, a, b);
+    s.z += a + b;
+    unpack2(w2, a, b);
+    s.w += a + b;
+    z2 = w2 = splat2(0.f);
+  };
+  // A vector of elements e.. of the row.  Some six instructions an element are what a bf16 row leaves room for beside its bytes, so the
+  // maximum and (bf16) the comparisons take two elements at a time, and what is rare stands apart.
   auto take = [&](const uint4& v, int e) {
-    float f[kN];
-    Vec<T>::get(v, f);
-    float top = f[0];
+    const float top = Vec<T>::top(v);
+    if (top > best) { best = top; best_e = e; }
+    if (top > s.m + kLag) { settle(); move_to(s, top); }
+    if (s.m > -1e38f) {
+      float f[kN];
+      Vec<T>::get(Vec<T>::floored(v), f);          // (0 * -inf would be a NaN)
+      const f32x2 mm = splat2(-s.m), c = splat2(kLog2e);
 #pragma unroll
-    for (int i = 1; i < kN; ++i) top = fmaxf(top, f[i]);
-    if (top > s.m) move_to(s, top);
-    const float base = s.m == -CUDART_INF_F ? 0.f : s.m;
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const float d = (f[i] - base) * kLog2e, p = ex2(d);
-      s.z += p;
-      s.w = fmaf(p, fmaxf(d, -1e30f), s.w);       // (0 * -inf)
-      ahead += f[i] > xt ? 1 : 0;
+      for (int i = 0; i < kN / 2; ++i) {
+        const f32x2 d = add2(pack2(f[2 * i], f[2 * i + 1]), mm);
+        float a, b;
+        unpack2(mul2(d, c), a, b);
+        const f32x2 p = pack2(ex2(a), ex2(b));
+        z2 = add2(z2, p);
+        w2 = fma2(p, d, w2);
+      }
+    } else {
+      const float2 zw = careful_sums<T>(v, s.m == -CUDART_INF_F ? 0.f : s.m);
+      s.z += zw.x;
+      s.w += zw.y;
     }
-    if (given && (e <= token || xt != xt)) {       // equal ones count where they come first, and all numbers come before a NaN
-#pragma unroll
-      for (int i = 0; i < kN; ++i)
-        if (e + i < end) ahead += xt != xt ? (f[i] == f[i] || e + i < token) : (f[i] == xt && e + i < token);
-    }
+    // what comes before the given token: larger ones, in front of it equal ones too
+    ahead2 += Vec<T>::above(v, e < token ? xb : xt);
   };
   const int step = kThreads * kN;
-  int e = begin + tid * kN;
-  for (; e + (kFly - 1) * step < end; e += kFly * step) {
+  int since = 0;
+#pragma unroll 1
+  for (int e = begin + tid * kN; e < end; e += kFly * step) {
     uint4 v[kFly];
 #pragma unroll
-    for (int i = 0; i < kFly; ++i) v[i] = load_vec(P, row, e + i * step, end);
+    for (int i = 0; i < kFly; ++i)
+      if (e + i * step < end) v[i] = load_vec<T, kWhole>(P, row, e + i * step, end);
 #pragma unroll
-    for (int i = 0; i < kFly; ++i) take(v[i], e + i * step);
+    for (int i = 0; i < kFly; ++i)
+      if (e + i * step < end) take(v[i], e + i * step);
+    if (++since == 4000 / kFly) {                  // (a half of the count takes four of a vector)
+      ahead += Vec<T>::kLow ? int(ahead2 & 0xffffu) + int(ahead2 >> 16) : int(ahead2);
+      ahead2 = 0u;
+      since = 0;
+    }
   }
-  for (; e < end; e += step) take(load_vec(P, row, e, end), e);
+  ahead += Vec<T>::kLow ? int(ahead2 & 0xffffu) + int(ahead2 >> 16) : int(ahead2);
+  if (given && begin <= token && token < end && tid == (token - begin) / kN % kThreads) {
+    // in the given token's own vector: it and its equals behind it have been counted, unless the vector begins with it
+    const int e = token - (token - begin) % kN;
+    for (int i = token; i < min(e + kN, end); ++i) ahead -= e < token && Vec<T>::one(row, i) == xt ? 1 : 0;
+  }
+  if (strange) {
+    ahead = 0;
+    for (int i = begin + tid; i < end; i += kThreads) {
+      const float x = Vec<T>::one(row, i);
+      ahead += xt != xt ? (x == x || i < token) : (x > xt || (x == xt && i < token));
+    }
+  }
+  settle();
 
   // ---- the CTA's sums; groups' largest elements
-  const float mine = s.m;
+  float most = best;
+  float m = s.m;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    const Stats b = {__shfl_xor_sync(0xffffffffu, s.m, o), __shfl_xor_sync(0xffffffffu, s.z, o), __shfl_xor_sync(0xffffffffu, s.w, o)};
-    s = joined(s, b);
+    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+  }
+  move_to(s, m);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    s.z += __shfl_xor_sync(0xffffffffu, s.z, o);
+    s.w += __shfl_xor_sync(0xffffffffu, s.w, o);
   }
   ahead = __reduce_add_sync(0xffffffffu, ahead);
-  if (lane == 0) { warp_stats[warp] = s; warp_ahead[warp] = ahead; }
+  if (lane == 0) { warp_stats[warp] = s; warp_ahead[warp] = ahead; warp_most[warp] = most; }
   if (tid == 0) n_cand = 0;
-  if (P.top > 0) {
+  if (P.top > 1) {
     constexpr int kGroup = kThreads / 64;          // threads of a group
-    float g = mine;
+    float g = best;
 #pragma unroll
     for (int o = kGroup / 2; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
     if (tid % kGroup == 0) group_top[tid / kGroup] = g;
@@ -188,6 +321,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const __grid_c
   if (tid == 0) {
     Stats a = warp_stats[0];
     int n = warp_ahead[0];
+#pragma unroll 1
     for (int w = 1; w < kWarps; ++w) { a = joined(a, warp_stats[w]); n += warp_ahead[w]; }
     if (kSplit == 1) { all_stats[0] = a; all_ahead[0] = n; }
     else {
@@ -199,38 +333,41 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const __grid_c
     }
   }
   if (P.top > 0) {
-    if (warp == kWarps - 1) {                      // the K-th largest of the 64
-      const float a = group_top[lane], b = group_top[lane + 32];
-      int na = 0, nb = 0;                          // groups ahead of mine, ties by place
+    float least = -CUDART_INF_F;
+    if (P.top == 1) {
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) least = fmaxf(least, warp_most[w]);
+    } else {
+      if (warp == kWarps - 1) {                    // the K-th largest of the 64
+        const float a = group_top[lane], b = group_top[lane + 32];
+        int na = 0, nb = 0;                        // groups ahead of mine, ties by place
 #pragma unroll 8
-      for (int i = 0; i < 64; ++i) {
-        const float x = group_top[i];
-        na += x > a || (x == a && i < lane) ? 1 : 0;
-        nb += x > b || (x == b && i < lane + 32) ? 1 : 0;
-      }
-      if (na == P.top - 1) bound = a;
-      if (nb == P.top - 1) bound = b;
-    }
-    __syncthreads();
-    const float least = bound;
-    if (least > -CUDART_INF_F) {
-      auto pick = [&](const uint4& v, int at) {
-        float f[kN];
-        Vec<T>::get(v, f);
-        float top = f[0];
-#pragma unroll
-        for (int i = 1; i < kN; ++i) top = fmaxf(top, f[i]);
-        if (top >= least) {
-#pragma unroll
-          for (int i = 0; i < kN; ++i)
-            if (f[i] >= least && at + i < end) {
-              const int n = atomicAdd(&n_cand, 1);
-              if (n < kCand) cand[n] = key_of(f[i], at + i);
-            }
+        for (int i = 0; i < 64; ++i) {
+          const float x = group_top[i];
+          na += x > a || (x == a && i < lane) ? 1 : 0;
+          nb += x > b || (x == b && i < lane + 32) ? 1 : 0;
         }
-      };
-      if (mine >= least) {                         // (a thread whose own largest is below has none)
-        for (int at = begin + tid * kN; at < end; at += step) pick(load_vec(P, row, at, end), at);
+        if (na == P.top - 1) bound = a;
+        if (nb == P.top - 1) bound = b;
+      }
+      __syncthreads();
+      least = bound;
+    }
+    if (least > -CUDART_INF_F) {
+      if (best >= least) {                         // (a thread whose own largest is below has none)
+        if (P.top == 1) pick<T>(load_vec<T, kWhole>(P, row, best_e, end), best_e, end, least, &n_cand, cand);         // (equal ones in later vectors come later)
+        else {
+#pragma unroll 1
+          for (int at = begin + tid * kN; at < end; at += kFly * step) {
+            uint4 v[kFly];
+#pragma unroll
+            for (int i = 0; i < kFly; ++i)
+              if (at + i * step < end) v[i] = load_vec<T, kWhole>(P, row, at + i * step, end);
+#pragma unroll
+            for (int i = 0; i < kFly; ++i)
+              if (at + i * step < end) pick<T>(v[i], at + i * step, end, least, &n_cand, cand);
+          }
+        }
       }
       __syncthreads();
     }
@@ -279,13 +416,13 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const __grid_c
   if (tid == 0) {
     Stats a = all_stats[0];
     int n = all_ahead[0];
-#pragma unroll
+#pragma unroll 1
     for (int i = 1; i < kSplit; ++i) { a = joined(a, all_stats[i]); n += all_ahead[i]; }
     const bool empty = a.m == -CUDART_INF_F && a.z == 0.f;
     const float log2z = log2f(a.z);
     const float lse = empty ? CUDART_INF_F : a.m + log2z * kLn2;
     lse_s = lse;
-    if (P.entropy) P.entropy[r] = empty ? 0.f : kLn2 * (log2z - a.w / a.z);
+    if (P.entropy) P.entropy[r] = empty ? 0.f : kLn2 * log2z - a.w / a.z;
     if (P.logprob) P.logprob[r] = !given ? 0.f : empty ? -CUDART_INF_F : (xt - a.m) - log2z * kLn2;
     if (P.rank) P.rank[r] = given ? n + 1 : 0;
     warp_stats[0] = {a.m, log2z * kLn2, empty ? 1.f : 0.f};
@@ -304,7 +441,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const __grid_c
         const int ip = i / P.top, ik = i - ip * P.top;
         const uint64_t key = all_top[ip][ik];
         int before = ik;                           // a part's own are in order
-#pragma unroll
+#pragma unroll 1
         for (int p = 0; p < kSplit; ++p)
           if (p != ip)
             for (int k = 0; k < P.top && (all_top[p][k] > key || (all_top[p][k] == key && p < ip)); ++k) ++before;
@@ -314,9 +451,13 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const __grid_c
   }
 }
 
-template <typename T, int kThreads, int kSplit>
+template <typename T, int kSplit>
 repq_status launch(const Params& P, cudaStream_t st) {
-  REPQ_CUDA(launch_chained_cluster(token_logprobs_kernel<T, kThreads, kSplit>, dim3(unsigned(P.rows) * kSplit), dim3(kThreads), 0, st, kSplit, P));
+  constexpr int kThreads = kSplit == 1 ? 128 : 256;      // (what a row costs beside its elements is per warp)
+  const bool whole = P.vec && P.vocab % Vec<T>::kN == 0;
+  const dim3 grid(unsigned(P.rows) * kSplit), block(kThreads);
+  if (whole) REPQ_CUDA(launch_chained_cluster(token_logprobs_kernel<T, kThreads, kSplit, true>, grid, block, 0, st, kSplit, P));
+  else REPQ_CUDA(launch_chained_cluster(token_logprobs_kernel<T, kThreads, kSplit, false>, grid, block, 0, st, kSplit, P));
   note_launch();
   return REPQ_OK;
 }
@@ -328,10 +469,10 @@ repq_status choose(Params& P, cudaStream_t st) {
   while (split < kMostSplit && P.rows * split * 2 <= 2 * sm_count() && P.vocab / (split * 2) >= 1024) split *= 2;
   P.per = int(round_up((P.vocab + split - 1) / split, 8));
   switch (split) {
-    case 1: return launch<T, 256, 1>(P, st);
-    case 2: return launch<T, 256, 2>(P, st);
-    case 4: return launch<T, 256, 4>(P, st);
-    default: return launch<T, 256, 8>(P, st);
+    case 1: return launch<T, 1>(P, st);
+    case 2: return launch<T, 2>(P, st);
+    case 4: return launch<T, 4>(P, st);
+    default: return launch<T, 8>(P, st);
   }
 }
 
