@@ -172,25 +172,24 @@ static __device__ __noinline__ uint2 exact_codes(float4 a, float4 b, float s) {
                     exact_code(b.x, s) | exact_code(b.y, s) << 8 | exact_code(b.z, s) << 16 | exact_code(b.w, s) << 24);
 }
 // ... of eight elements: x * (1 / s) is within 2^-15 of the quotient where codes are, so only pieces with a value near a tie (or an infinity
-// or NaN) are divided, one in 150; all other roundings are those of the float adder (1.5 * 2^23 + 128, whose low byte is the code).
+// or NaN) are divided, one in some 600; all other roundings are those of the float adder (1.5 * 2^23 + 128, whose low byte is the code).
 // (A division of every element inlined: 38 instructions an element, 49 us for what takes 9 at the memory's rate.)
 __device__ __forceinline__ uint2 codes_of(const float (&f)[8], float s, float inv) {
   constexpr float kMagic = 12582912.f + 128.f;
   const f32x2 inv2 = splat2(inv), up = splat2(kMagic), down = splat2(-kMagic);
   uint32_t u[8];
-  bool plain = true;
+  float far = 0.f;                                 // from the code, the farthest of them
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const f32x2 t = mul2(pack2(f[2 * k], f[2 * k + 1]), inv2), q = add2(t, up), back = add2(q, down);
-    float t0, t1, q0, q1, b0, b1;
-    unpack2(t, t0, t1);
+    const f32x2 t = mul2(pack2(f[2 * k], f[2 * k + 1]), inv2), q = add2(t, up), off = fma2(add2(q, down), splat2(-1.f), t);
+    float q0, q1, o0, o1;
     unpack2(q, q0, q1);
-    unpack2(back, b0, b1);
-    plain = plain && fabsf(t0 - b0) < 0.4999f && fabsf(t1 - b1) < 0.4999f;
+    unpack2(off, o0, o1);
+    asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(far) : "f"(fabsf(o0)), "f"(fabsf(o1)));
     u[2 * k] = __float_as_uint(q0);
     u[2 * k + 1] = __float_as_uint(q1);
   }
-  if (!plain) return exact_codes(make_float4(f[0], f[1], f[2], f[3]), make_float4(f[4], f[5], f[6], f[7]), s);
+  if (!(far < 0.4999f)) return exact_codes(make_float4(f[0], f[1], f[2], f[3]), make_float4(f[4], f[5], f[6], f[7]), s);
   return make_uint2(__byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410),
                     __byte_perm(__byte_perm(u[4], u[5], 0x0040), __byte_perm(u[6], u[7], 0x0040), 0x5410));
 }
@@ -228,7 +227,7 @@ template <> struct Piece<float> {
 };
 
 // A run's rows, by `kThreads` threads of which this is number `t`: a warp, or the whole CTA (`tops`: a word per warp in shared memory).
-template <typename T, int kThreads>
+template <typename T, int kThreads, bool kEven>
 __device__ __forceinline__ void write_run(const WriteParams& P, int head, int kv, int t0, int slot0, int rows, int t, uint32_t* tops) {
   const int lane = t & 31, bs = 1 << P.shift, off = slot0 & (bs - 1), page = slot0 >> P.shift;
   const int64_t tile = int64_t(page) * P.c.kv_heads + head;
@@ -237,11 +236,14 @@ __device__ __forceinline__ void write_run(const WriteParams& P, int head, int kv
   uint8_t* codes = (kv ? P.c.v_codes : P.c.k_codes) + (tile << P.shift) * P.c.d_h;
   float* scale = (kv ? P.c.v_scale : P.c.k_scale) + tile;
   const int n = rows * P.pieces;
+  // (kEven: the threads' pieces of a row are whole rows, so a thread's pieces lie at a fixed step)
+  const T* x0 = x + (t * P.by_pieces >> 16) * st + 8 * (t - (t * P.by_pieces >> 16) * P.pieces);
+  const int64_t step = (kThreads * P.by_pieces >> 16) * st;
   Piece<T> held[kHeld];
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
     const int e = t + kThreads * i;
-    if (e < n) { const int r = e * P.by_pieces >> 16; held[i].load(x + r * st + 8 * (e - r * P.pieces)); }
+    if (e < n) held[i].load(kEven ? x0 + i * step : x + (e * P.by_pieces >> 16) * st + 8 * (e - (e * P.by_pieces >> 16) * P.pieces));
     else held[i].clear();
   }
   const float before = off ? *scale : 0.f;
@@ -277,7 +279,8 @@ __device__ __forceinline__ void write_run(const WriteParams& P, int head, int kv
     if (kThreads > 32) __syncthreads();            // (every warp has read the scale)
     if (t == 0) *scale = after;
   }
-  const float inv = __fdiv_rn(1.0f, after);
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(after));
   uint2* to = reinterpret_cast<uint2*>(codes + off * P.c.d_h);
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
@@ -289,7 +292,7 @@ __device__ __forceinline__ void write_run(const WriteParams& P, int head, int kv
   }
 }
 
-template <typename T, int kThreads>
+template <typename T, int kThreads, bool kEven>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 768 / kThreads : 512 / kThreads) cache_write_kernel(const __grid_constant__ WriteParams P) {
   constexpr int kWarps = kThreads / 32, kFits = 32 * kHeld;             // pieces of a warp
   __shared__ uint32_t tops[2][kWarps];
@@ -328,10 +331,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 768 / kThreads : 51
         rows = min(rows, most);
       }
       if (rows * P.pieces <= kFits) {
-        if (nth++ % kWarps == warp) write_run<T, 32>(P, head, kv, t0, slot0, rows, lane, nullptr);
+        if (nth++ % kWarps == warp) write_run<T, 32, kEven>(P, head, kv, t0, slot0, rows, lane, nullptr);
       } else {
         // (two sets of words in turn: a warp may be a run ahead of those that still read)
-        write_run<T, kThreads>(P, head, kv, t0, slot0, rows, tid, tops[shared++ & 1]);
+        write_run<T, kThreads, kEven>(P, head, kv, t0, slot0, rows, tid, tops[shared++ & 1]);
       }
     }
   }
@@ -341,8 +344,11 @@ template <typename T>
 repq_status launch_write(const WriteParams& P, cudaStream_t st) {
   const dim3 grid((P.tokens + P.window - 1) / P.window, P.c.kv_heads, 2);
   // four warps hold 64 rows of 128 channels
-  if (P.shift <= 6) REPQ_CUDA(launch_chained(cache_write_kernel<T, 128>, grid, dim3(128), 0, st, P));
-  else REPQ_CUDA(launch_chained(cache_write_kernel<T, 256>, grid, dim3(256), 0, st, P));
+  const bool even = 32 % P.pieces == 0;
+  if (P.shift <= 6 && even) REPQ_CUDA(launch_chained(cache_write_kernel<T, 128, true>, grid, dim3(128), 0, st, P));
+  else if (P.shift <= 6) REPQ_CUDA(launch_chained(cache_write_kernel<T, 128, false>, grid, dim3(128), 0, st, P));
+  else if (even) REPQ_CUDA(launch_chained(cache_write_kernel<T, 256, true>, grid, dim3(256), 0, st, P));
+  else REPQ_CUDA(launch_chained(cache_write_kernel<T, 256, false>, grid, dim3(256), 0, st, P));
   note_launch();
   return REPQ_OK;
 }

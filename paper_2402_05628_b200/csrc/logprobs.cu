@@ -258,7 +258,9 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const __grid_c
       s.w += zw.y;
     }
     // what comes before the given token: larger ones, in front of it equal ones too
-    ahead2 += Vec<T>::above(v, e < token ? xb : xt);
+    // (few vectors have any where the token is a plausible one)
+    const float over = e < token ? xb : xt;
+    if (top > over) ahead2 += Vec<T>::above(v, over);
   };
   const int step = kThreads * kN;
   int since = 0;
