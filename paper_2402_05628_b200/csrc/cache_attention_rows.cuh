@@ -9,7 +9,7 @@
 // A warp multiplies on mma.m16n8k16 in f16 with float32 sums, keys and channels on the M side, rows on the N side:
 //     S^T [16 keys x 8 rows] = K [16 x d_h] Q^T,      O^T [d_h x 8 rows] += V^T [d_h x 16 keys] P^T.
 // Codes minus 128 are f16 numbers exactly.  The contraction's order is free, so a thread loads its operands straight from the
-// cache in 16-byte pieces (K: d_h / 4 consecutive bytes of two keys; V: d_h / 8 consecutive channels of four keys, transposed
+// cache in 16-byte pieces (K: d_h / 4 bytes of two keys; V: d_h / 8 consecutive channels of four keys, transposed
 // by byte permutations that the conversion needs anyway); nothing passes through shared memory until the end of a job.
 //
 // With x = S alpha k_scale log2 e, a row keeps m, the largest x + log2 v_scale seen, Z = sum 2^(x - m + 15) and
@@ -40,20 +40,21 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 __device__ __forceinline__ uint32_t pack_half(float a, float b) { return bits_of(__floats2half2_rn(a, b)); }
 __device__ __forceinline__ float2 unpack_half(uint32_t w) { return __half22float2(half2_of(w)); }
 
-// kWords consecutive words, by the widest loads their alignment (the step between threads) allows; the cache is read once
-template <int kWords> __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[kWords]) {
+// kWords words by the widest pieces that their number allows, pieces kApart bytes apart; the cache is read once
+constexpr int piece_of(int words) { return words % 4 == 0 ? 16 : words % 2 == 0 ? 8 : 4; }
+template <int kWords, int kApart> __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[kWords]) {
   if constexpr (kWords % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < kWords / 4; ++i)
       asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-                   : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3]) : "l"(p + 16 * i));
+                   : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3]) : "l"(p + kApart * i));
   } else if constexpr (kWords % 2 == 0) {
 #pragma unroll
     for (int i = 0; i < kWords / 2; ++i)
-      asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[2 * i]), "=r"(w[2 * i + 1]) : "l"(p + 8 * i));
+      asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[2 * i]), "=r"(w[2 * i + 1]) : "l"(p + kApart * i));
   } else {
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(w[i]) : "l"(p + 4 * i));
+    for (int i = 0; i < kWords; ++i) asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(w[i]) : "l"(p + kApart * i));
   }
 }
 
@@ -68,14 +69,16 @@ struct Keys {
     if (!there) return;
     constexpr int dh = 16 * kSteps;
     const int64_t tile = int64_t(page) * P.c.kv_heads + h;
-    const uint8_t* kp = P.c.k_codes + ((tile << P.shift) + off) * dh + g * dh + t * (4 * kSteps);
-    load_words<kSteps>(kp, k[0]);
-    load_words<kSteps>(kp + 8 * dh, k[1]);
+    // (piece i of the four lanes of a key row covers consecutive bytes: whole sectors)
+    constexpr int kPiece = piece_of(kSteps);
+    const uint8_t* kp = P.c.k_codes + ((tile << P.shift) + off) * dh + g * dh + t * kPiece;
+    load_words<kSteps, 4 * kPiece>(kp, k[0]);
+    load_words<kSteps, 4 * kPiece>(kp + 8 * dh, k[1]);
     const uint8_t* vp = P.c.v_codes + ((tile << P.shift) + off) * dh + 2 * t * dh + g * (2 * kSteps);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint8_t* p = vp + ((i & 1) + 8 * (i >> 1)) * dh;
-      if constexpr (kSteps % 2 == 0) load_words<kV>(p, v[i]);
+      if constexpr (kSteps % 2 == 0) load_words<kV, piece_of(kV)>(p, v[i]);
       else {
 #pragma unroll
         for (int j = 0; j < kV; ++j)
@@ -83,9 +86,15 @@ struct Keys {
                     (2 * j + 1 < kSteps ? uint32_t(__ldg(reinterpret_cast<const uint16_t*>(p) + 2 * j + 1)) << 16 : 0u);
       }
     }
-    ks = __ldg(P.c.k_scale + tile);
-    vs = __ldg(P.c.v_scale + tile);
+    asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(ks) : "l"(P.c.k_scale + tile));
+    asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(vs) : "l"(P.c.v_scale + tile));
   }
+};
+
+// A stretch of the line that lies in one job: units [u0, u1) of the keys that rows row0.. of a request and key / value head h see.
+struct Job {
+  int b, h, row0, n_rows, q0, before, kv, u0, u1, units;     // n_rows: of the request; before: tokens ahead of its first query
+  long long at;                                               // of the job's first unit on the line
 };
 
 // A warp's rows: queries as B fragments, running statistics of its columns, accumulators.
@@ -96,21 +105,24 @@ struct Rows {
   float m[kTiles][2], z[kTiles][2];
   float o[kTiles][kSteps][4];
   int limit[kTiles][2];                           // keys that the column's row sees
+  int all_see;                                    // keys that every row of the warp sees
 
   template <typename T>
-  __device__ __forceinline__ void load_row(const AttendParams& P, const Request& rq, int h, int row, int n_rows, int t, int i, float& factor) {
+  __device__ __forceinline__ void load_row(const AttendParams& P, const volatile Job& J, int row, int t, int i, float& factor) {
+    constexpr int kPiece = piece_of(kSteps);       // channels as the keys' pieces lie: word j of a thread begins at channel ...
+    constexpr auto channel = [](int j) { return 4 * j / kPiece * 4 * kPiece + 4 * j % kPiece; };
     float f[4 * kSteps];
     const int token = row / P.group;
-    const T* p = static_cast<const T*>(P.q) + (rq.q0 + token) * P.q_st + (h * P.group + row - token * P.group) * P.q_sh + t * (4 * kSteps);
-    const bool in = row < n_rows;
+    const T* p = static_cast<const T*>(P.q) + (J.q0 + token) * P.q_st + (J.h * P.group + row - token * P.group) * P.q_sh + t * kPiece;
+    const bool in = row < J.n_rows;
     float top = 0.f;
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) {
       if constexpr (sizeof(T) == 4) {
-        const float4 w = in ? __ldg(reinterpret_cast<const float4*>(p) + j) : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float4 w = in ? __ldg(reinterpret_cast<const float4*>(p + channel(j))) : make_float4(0.f, 0.f, 0.f, 0.f);
         f[4 * j] = w.x; f[4 * j + 1] = w.y; f[4 * j + 2] = w.z; f[4 * j + 3] = w.w;
       } else {
-        const uint2 w = in ? __ldg(reinterpret_cast<const uint2*>(p) + j) : make_uint2(0u, 0u);
+        const uint2 w = in ? __ldg(reinterpret_cast<const uint2*>(p + channel(j))) : make_uint2(0u, 0u);
         f[4 * j] = __uint_as_float(w.x << 16); f[4 * j + 1] = __uint_as_float(w.x & 0xffff0000u);
         f[4 * j + 2] = __uint_as_float(w.y << 16); f[4 * j + 3] = __uint_as_float(w.y & 0xffff0000u);
       }
@@ -134,19 +146,21 @@ struct Rows {
     }
   }
 
-  __device__ __forceinline__ void begin(const AttendParams& P, const Request& rq, int h, int row0, int n_rows, int g, int t) {
+  __device__ __forceinline__ void begin(const AttendParams& P, const volatile Job& J, int g, int t) {
+    const int row0 = J.row0, n_rows = J.n_rows, before = J.before;
+    all_see = min(before + row0 / P.group + 1, P.max_kv);
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
       float factor;
       const int row = row0 + 8 * i + g;
-      if constexpr (kPrecise) load_row<float>(P, rq, h, row, n_rows, t, i, factor);
-      else load_row<__nv_bfloat16>(P, rq, h, row, n_rows, t, i, factor);
+      if constexpr (kPrecise) load_row<float>(P, J, row, t, i, factor);
+      else load_row<__nv_bfloat16>(P, J, row, t, i, factor);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         back[i][c] = __shfl_sync(0xffffffffu, factor, 4 * (2 * t + c));     // (lane of row 2 t + c)
         const int col = row0 + 8 * i + 2 * t + c;
-        limit[i][c] = col < n_rows ? min(rq.kv - rq.q_true + col / P.group + 1, P.max_kv) : 0;
-        m[i][c] = -CUDART_INF_F;
+        limit[i][c] = col < n_rows ? min(before + col / P.group + 1, P.max_kv) : 0;
+        m[i][c] = col < n_rows ? -CUDART_INF_F : CUDART_INF_F;               // (columns of no row have no weights and never rise)
         z[i][c] = 0.f;
       }
 #pragma unroll
@@ -159,20 +173,24 @@ struct Rows {
   // 16 keys from k0 on
   __device__ __forceinline__ void take(const Keys<kSteps>& K, int k0, int g) {
     if (!K.there) return;
-    float s[kTiles][4];
+    float s[kTiles][4], s2[kTiles][4];             // (two chains: an MMA waits for the one before it in its chain)
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[i][e] = 0.f;
+      for (int e = 0; e < 4; ++e) s[i][e] = s2[i][e] = 0.f;
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) {
       const uint32_t a[4] = {codes_lo(K.k[0][j]), codes_lo(K.k[1][j]), codes_hi(K.k[0][j]), codes_hi(K.k[1][j])};
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) {
-        mma(s[i], a, q[i][2 * j], q[i][2 * j + 1]);
-        if constexpr (kPrecise) mma(s[i], a, ql[i][2 * j], ql[i][2 * j + 1]);
+        mma(j & 1 ? s2[i] : s[i], a, q[i][2 * j], q[i][2 * j + 1]);
+        if constexpr (kPrecise) mma(j & 1 ? s[i] : s2[i], a, ql[i][2 * j], ql[i][2 * j + 1]);
       }
     }
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[i][e] += s2[i][e];
     const float lvs = lg2(K.vs);
     bool rises = false;
 #pragma unroll
@@ -180,8 +198,12 @@ struct Rows {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const float f = K.ks * back[i][c];
-        s[i][c] = k0 + g < limit[i][c] ? s[i][c] * f : -CUDART_INF_F;
-        s[i][2 + c] = k0 + 8 + g < limit[i][c] ? s[i][2 + c] * f : -CUDART_INF_F;
+        s[i][c] *= f;
+        s[i][2 + c] *= f;
+        if (k0 + 16 > all_see) {
+          if (k0 + g >= limit[i][c]) s[i][c] = -CUDART_INF_F;
+          if (k0 + 8 + g >= limit[i][c]) s[i][2 + c] = -CUDART_INF_F;
+        }
         rises = rises || fmaxf(s[i][c], s[i][2 + c]) + lvs > m[i][c];
       }
     if (__any_sync(0xffffffffu, rises)) {
@@ -251,6 +273,7 @@ struct Shared {
   float m[kWarps][kRows], z[kWarps][kRows];
   int sums[kRows];
   long long first[kThreads + 1];                  // units before a thread's requests
+  Job job[2][kWarps];                             // this job and the next, every warp's own copy
   int last;
 };
 
@@ -265,7 +288,7 @@ __device__ __forceinline__ Share share_of(const AttendParams& P, const Request& 
 }
 
 template <int kSteps, int kTiles, bool kPrecise>
-__global__ void __launch_bounds__(kThreads, kTiles == 1 && !kPrecise ? 4 : 3) cache_rows_kernel(const __grid_constant__ AttendParams P) {
+__global__ void __launch_bounds__(kThreads, kTiles == 1 && !kPrecise && kSteps < 7 ? 4 : 3) cache_rows_kernel(const __grid_constant__ AttendParams P) {
   constexpr int kRowsOf = 8 * kTiles, dh = 16 * kSteps, kPart = kRowsOf * (dh + 2);
   __shared__ Shared<kSteps, kTiles> S;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -313,40 +336,81 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 && !kPrecise ? 4 : 3) ca
   }
   Request rq = request_of(P, b);
   Share sh = share_of(P, rq, kRowsOf);
-  while (at < end) {
+  // the stretch that begins at `at`, for the warp's own copy
+  auto find = [&](volatile Job& J) {
     while (at >= start + (long long)sh.tiles * sh.units * P.c.kv_heads) {
       start += (long long)sh.tiles * sh.units * P.c.kv_heads;
       rq = request_of(P, ++b);
       sh = share_of(P, rq, kRowsOf);
     }
     const int job = int((at - start) / sh.units), u0 = int(at - start - (long long)job * sh.units);
-    const int u1 = int(min((long long)sh.units, u0 + (end - at)));
-    const int h = job / sh.tiles, row0 = (job - h * sh.tiles) * kRowsOf, n_rows = rq.q_len * P.group, live = min(n_rows - row0, kRowsOf);
+    if (lane == 0) {
+      J.b = b;
+      J.h = job / sh.tiles;
+      J.row0 = (job - job / sh.tiles * sh.tiles) * kRowsOf;
+      J.n_rows = rq.q_len * P.group;
+      J.q0 = rq.q0;
+      J.before = rq.kv - rq.q_true;
+      J.kv = rq.kv;
+      J.u0 = u0;
+      J.u1 = int(min((long long)sh.units, u0 + (end - at)));
+      J.units = sh.units;
+      J.at = start + (long long)job * sh.units;
+    }
+    __syncwarp();
+    at += min((long long)sh.units - u0, end - at);
+  };
+  // the block of the warp's 16 keys in unit u, -1 past the stretch or what the tile's last row sees
+  auto seen_by = [&](const volatile Job& J) {
+    const int live = min(J.n_rows - J.row0, kRowsOf);
+    return min(min(J.before + (J.row0 + live - 1) / P.group + 1, J.kv), P.max_kv);
+  };
+  auto page_of = [&](const int32_t* table, int u, int u1, int seen) {
+    const int k0 = u * kUnit + 16 * warp;
+    int page = -1;
+    if (u < u1 && k0 < seen) asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(page) : "l"(table + (k0 >> P.shift)));
+    return page;
+  };
+  auto off_of = [&](int u) { return (u * kUnit + 16 * warp) & ((1 << P.shift) - 1); };
 
+  // The first keys of a stretch are asked for before the one ahead of it is joined, and where they lie is found while that one's first
+  // keys are on their way.
+  find(S.job[0][warp]);
+  Keys<kSteps> A, B;
+  {
+    const volatile Job& J = S.job[0][warp];
+    A.load(P, page_of(P.table + J.b * P.ld_table, J.u0, J.u1, seen_by(J)), J.h, off_of(J.u0), g, t);
+  }
+  for (int turn = 0;; turn ^= 1) {
+    const volatile Job& J = S.job[turn][warp];
+    const bool more = at < end;
+    int next_page = -1;
     Rows<kSteps, kTiles, kPrecise> R;
-    R.begin(P, rq, h, row0, n_rows, g, t);
-    // keys that the tile's last row sees, within the table
-    const int seen = min(min(rq.kv - rq.q_true + (row0 + live - 1) / P.group + 1, rq.kv), P.max_kv);
     {
-      const int32_t* table = P.table + b * P.ld_table;
-      auto page_of = [&](int u) {
-        const int k0 = u * kUnit + 16 * warp;
-        return u < u1 && k0 < seen ? __ldg(table + (k0 >> P.shift)) : -1;
-      };
-      auto off_of = [&](int u) { return (u * kUnit + 16 * warp) & ((1 << P.shift) - 1); };
-      Keys<kSteps> A, B;
-      A.load(P, page_of(u0), h, off_of(u0), g, t);
-      int next = page_of(u0 + 1);
+      const int32_t* table = P.table + J.b * P.ld_table;
+      const int h = J.h, u1 = J.u1, seen = seen_by(J);
+      int u = J.u0, next = page_of(table, u + 1, u1, seen);
+      R.begin(P, J, g, t);
+      if (more) {
+        volatile Job& N = S.job[turn ^ 1][warp];
+        find(N);
+        next_page = page_of(P.table + N.b * P.ld_table, N.u0, N.u1, seen_by(N));
+      }
 #pragma unroll 1
-      for (int u = u0; u < u1; u += 2) {
+      for (; u < u1; u += 2) {
         B.load(P, next, h, off_of(u + 1), g, t);
-        next = page_of(u + 2);
+        next = page_of(table, u + 2, u1, seen);
         R.take(A, u * kUnit + 16 * warp, g);
         A.load(P, next, h, off_of(u + 2), g, t);
-        next = page_of(u + 3);
+        next = page_of(table, u + 3, u1, seen);
         R.take(B, (u + 1) * kUnit + 16 * warp, g);
       }
     }
+    if (more) {
+      const volatile Job& N = S.job[turn ^ 1][warp];
+      A.load(P, next_page, N.h, off_of(N.u0), g, t);
+    }
+    const int h = J.h, row0 = J.row0, q0 = J.q0, live = min(J.n_rows - row0, kRowsOf);
 
     // ---- the warps' sums joined
 #pragma unroll
@@ -365,13 +429,13 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 && !kPrecise ? 4 : 3) ca
       }
     if (tid < kRowsOf) S.sums[tid] = 0;
     __syncthreads();
-    const bool whole = u0 == 0 && u1 == sh.units;
-    const long long job_at = start + (long long)job * sh.units;
-    const int w0 = int(((job_at + 1) * workers - 1) / total), w1 = int(((job_at + sh.units) * workers - 1) / total);
+    const bool whole = J.u0 == 0 && J.u1 == J.units;
+    const long long job_at = J.at;
+    const int w0 = int(((job_at + 1) * workers - 1) / total), w1 = int(((job_at + J.units) * workers - 1) / total);
     auto part_of = [&](int w) { return P.partials + (2 * w + (w == w0 ? 1 : 0)) * int64_t(kPart); };
     float* mine = part_of(blockIdx.x);
     auto put_row = [&](int row, int d, float a, float b2, float m, float z) {
-      const int r = row0 + row, token = rq.q0 + r / P.group, head = h * P.group + r % P.group;
+      const int r = row0 + row, token = q0 + r / P.group, head = h * P.group + r % P.group;
       const float inv = z > 0.f ? __fdividef(1.f, z) : z == 0.f ? 0.f : CUDART_NAN_F;
       const int sum = store_pair(P, token, head, d, a * inv, b2 * inv);
       if (P.out_row_sum) atomicAdd(&S.sums[row], sum);
@@ -431,8 +495,8 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 && !kPrecise ? 4 : 3) ca
       }
     }
     __syncthreads();
-    if (writes && P.out_row_sum && tid < live) atomicAdd(P.out_row_sum + rq.q0 + (row0 + tid) / P.group, S.sums[tid]);
-    at += u1 - u0;
+    if (writes && P.out_row_sum && tid < live) atomicAdd(P.out_row_sum + q0 + (row0 + tid) / P.group, S.sums[tid]);
+    if (!more) break;
     __syncthreads();
   }
 }
