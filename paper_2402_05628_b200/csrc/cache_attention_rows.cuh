@@ -274,7 +274,7 @@ struct Shared {
   int sums[kRows];
   long long first[kThreads + 1];                  // units before a thread's requests
   Job job[2][kWarps];                             // this job and the next, every warp's own copy
-  int last;
+  int last, cost;
 };
 
 // units of 64 keys that the tiles of one key / value head of a request take
@@ -287,6 +287,11 @@ __device__ __forceinline__ Share share_of(const AttendParams& P, const Request& 
   return s;
 }
 
+// A job costs a share as much as so many units beside its own: its queries, the join of its warps, its output.  Where lengths differ, shares of
+// many short jobs would otherwise be the last to end (64 requests of 1 to 4096 tokens: 84 us without, ... with).  Calls of few units deal
+// out bare units.
+constexpr int kJobCost = 2;
+
 template <int kSteps, int kTiles, bool kPrecise>
 __global__ void __launch_bounds__(kThreads, kTiles == 1 && !kPrecise && kSteps < 7 ? 4 : 3) cache_rows_kernel(const __grid_constant__ AttendParams P) {
   constexpr int kRowsOf = 8 * kTiles, dh = 16 * kSteps, kPart = kRowsOf * (dh + 2);
@@ -298,26 +303,34 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 && !kPrecise && kSteps <
   // ---- the line of units: requests in order, of one the key / value heads, of one the row tiles
   const int per = (P.requests + kThreads - 1) / kThreads;
   {
-    long long n = 0;
+    long long n = 0, jobs = 0;
     for (int b = tid * per; b < min((tid + 1) * per, P.requests); ++b) {
       const Share s = share_of(P, request_of(P, b), kRowsOf);
       n += (long long)s.tiles * s.units * P.c.kv_heads;
+      jobs += (long long)s.tiles * P.c.kv_heads;
     }
-    long long before = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long a = __shfl_up_sync(0xffffffffu, before, o);
-      if (lane >= o) before += a;
+      const long long a = __shfl_up_sync(0xffffffffu, n, o), c = __shfl_up_sync(0xffffffffu, jobs, o);
+      if (lane >= o) { n += a; jobs += c; }
     }
-    if (lane == 31) S.first[warp] = before;       // (warps' sums for a moment)
+    if (lane == 31) { S.first[warp] = n; S.first[kWarps + warp] = jobs; }     // (warps' sums for a moment)
     __syncthreads();
-    for (int w = 0; w < warp; ++w) before += S.first[w];
+    long long all = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const long long a = S.first[w];
+      all += a;
+      if (w < warp) { n += a; jobs += S.first[kWarps + w]; }
+    }
     __syncthreads();
-    S.first[tid + 1] = before;
-    if (tid == 0) S.first[0] = 0;
+    const int c = all >= 4 * (long long)gridDim.x ? kJobCost : 0;
+    S.first[tid + 1] = n + c * jobs;
+    if (tid == 0) { S.first[0] = 0; S.cost = c; }
     __syncthreads();
   }
   const long long total = S.first[kThreads];
+  const int cost = S.cost;
   const long long workers = min((long long)gridDim.x, total);
   if (blockIdx.x >= workers) return;
   long long at = blockIdx.x * total / workers;
@@ -336,29 +349,36 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 && !kPrecise && kSteps <
   }
   Request rq = request_of(P, b);
   Share sh = share_of(P, rq, kRowsOf);
-  // the stretch that begins at `at`, for the warp's own copy
+  // the next stretch of units from `at` on, for the warp's own copy; false: the share has no more
   auto find = [&](volatile Job& J) {
-    while (at >= start + (long long)sh.tiles * sh.units * P.c.kv_heads) {
-      start += (long long)sh.tiles * sh.units * P.c.kv_heads;
-      rq = request_of(P, ++b);
-      sh = share_of(P, rq, kRowsOf);
+    while (at < end) {
+      const int each = sh.units + cost;
+      if (at >= start + (long long)sh.tiles * each * P.c.kv_heads) {
+        start += (long long)sh.tiles * each * P.c.kv_heads;
+        rq = request_of(P, ++b);
+        sh = share_of(P, rq, kRowsOf);
+        continue;
+      }
+      const int job = int((at - start) / each), o0 = int(at - start - (long long)job * each), o1 = int(min((long long)each, o0 + (end - at)));
+      at += o1 - o0;
+      if (o1 <= cost) continue;                   // (none of its units)
+      if (lane == 0) {
+        J.b = b;
+        J.h = job / sh.tiles;
+        J.row0 = (job - job / sh.tiles * sh.tiles) * kRowsOf;
+        J.n_rows = rq.q_len * P.group;
+        J.q0 = rq.q0;
+        J.before = rq.kv - rq.q_true;
+        J.kv = rq.kv;
+        J.u0 = max(o0 - cost, 0);
+        J.u1 = o1 - cost;
+        J.units = sh.units;
+        J.at = start + (long long)job * each + cost;
+      }
+      __syncwarp();
+      return true;
     }
-    const int job = int((at - start) / sh.units), u0 = int(at - start - (long long)job * sh.units);
-    if (lane == 0) {
-      J.b = b;
-      J.h = job / sh.tiles;
-      J.row0 = (job - job / sh.tiles * sh.tiles) * kRowsOf;
-      J.n_rows = rq.q_len * P.group;
-      J.q0 = rq.q0;
-      J.before = rq.kv - rq.q_true;
-      J.kv = rq.kv;
-      J.u0 = u0;
-      J.u1 = int(min((long long)sh.units, u0 + (end - at)));
-      J.units = sh.units;
-      J.at = start + (long long)job * sh.units;
-    }
-    __syncwarp();
-    at += min((long long)sh.units - u0, end - at);
+    return false;
   };
   // the block of the warp's 16 keys in unit u, -1 past the stretch or what the tile's last row sees
   auto seen_by = [&](const volatile Job& J) {
@@ -375,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 && !kPrecise && kSteps <
 
   // The first keys of a stretch are asked for before the one ahead of it is joined, and where they lie is found while that one's first
   // keys are on their way.
-  find(S.job[0][warp]);
+  if (!find(S.job[0][warp])) return;
   Keys<kSteps> A, B;
   {
     const volatile Job& J = S.job[0][warp];
@@ -383,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 && !kPrecise && kSteps <
   }
   for (int turn = 0;; turn ^= 1) {
     const volatile Job& J = S.job[turn][warp];
-    const bool more = at < end;
+    bool more;
     int next_page = -1;
     Rows<kSteps, kTiles, kPrecise> R;
     {
@@ -391,9 +411,9 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 && !kPrecise && kSteps <
       const int h = J.h, u1 = J.u1, seen = seen_by(J);
       int u = J.u0, next = page_of(table, u + 1, u1, seen);
       R.begin(P, J, g, t);
+      volatile Job& N = S.job[turn ^ 1][warp];
+      more = find(N);
       if (more) {
-        volatile Job& N = S.job[turn ^ 1][warp];
-        find(N);
         next_page = page_of(P.table + N.b * P.ld_table, N.u0, N.u1, seen_by(N));
       }
 #pragma unroll 1
