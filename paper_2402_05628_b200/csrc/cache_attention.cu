@@ -63,6 +63,7 @@ repq_status route_of(AttendParams& P, bool precise, Route* out) {
   else {
     // as many tokens as max_q_len allows: every request is a chunk
     r.chunks = true;
+    REPQ_REQUIRE((int64_t(P.max_kv) / 128 + 4) * P.c.kv_heads < (int64_t(1) << 31), REPQ_UNSUPPORTED, "repq_cache_attention: max_kv_len %d", P.max_kv);
     r.rows = int64_t(P.tokens) != int64_t(P.requests) * P.max_q;
     r.few = r.rows ? kFewRows : 0;
   }
@@ -85,9 +86,9 @@ repq_status route_of(AttendParams& P, bool precise, Route* out) {
 ChunksPlan chunks_plan(const AttendParams& P) {
   ChunksPlan plan;
   plan.ctas = sm_count();
-  // two counters for the items, two per item that is cut along the keys (at most half as many items as CTAs), and a part per CTA then
-  plan.counter_bytes = size_t(round_up(4 * (2 + int64_t(plan.ctas)), 256));
-  plan.workspace = plan.counter_bytes + size_t(plan.ctas) * 256 * (P.c.d_h + 2) * sizeof(float);
+  // per CTA two counters (of the item that its share ends in, a tile each) and two parts of two tiles
+  plan.counter_bytes = size_t(round_up(8 * int64_t(plan.ctas), 256));
+  plan.workspace = plan.counter_bytes + size_t(plan.ctas) * 4 * 128 * (P.c.d_h + 2) * sizeof(float);
   return plan;
 }
 

@@ -11,9 +11,9 @@
 // the sum is Z = sum w / v_scale, a product per 16 keys.  m follows the largest x + lv of the row at a distance of up to 8, so w
 // is at most 2^15 and the accumulator is rescaled rarely; weights have 11 bits down to 2^-21 of the largest.
 //
-// Items (request, row pair, head; the longest of a request first) are handed out by a counter; where there are fewer of them than SMs, each
-// is cut along the keys and joined by the part that finishes last, parts in order.
-// Roles: two groups of four softmax warps, four conversion warps, a warp per tile that issues MMAs, one that fetches items.  Every wait is
+// Items (request, row pair, head) form one line, an item as long as its steps of 128 keys and some more for what it costs beside them, cut into
+// equal shares for the CTAs; an item that lies in several shares is joined by whichever CTA finishes last, parts in order.
+// Roles: two groups of four softmax warps, four conversion warps, a warp per tile that issues MMAs, one that finds items.  Every wait is
 // bounded; when one runs out all roles leave, MMAs in flight are drained and tensor memory is freed.
 #pragma once
 #include <type_traits>
@@ -38,13 +38,15 @@ constexpr int kSoftRegs = 176, kConvRegs = 80, kOtherRegs = 80;
 constexpr float kLift = 7.f, kLag = 8.f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// before: tokens ahead of the request's first query; j0: its first step of 128 keys; ends: steps of 64 keys of its two tiles, from there
-struct Item { int b, h, row0, q0, before, n_rows, j0, ends[2], part, id; };
+// before: tokens ahead of the request's first query; j0: its first step of 128 keys; ends: steps of 64 keys of its two tiles, from
+// there; w0, parts: the first of the CTAs that share it, and their number
+struct Item { int b, h, row0, q0, before, n_rows, j0, ends[2], w0, parts; };
+constexpr int kItemCost = 2;             // steps
+constexpr int kLeastShare = 4;           // positions of a CTA
 
 struct ChunkParams {
   AttendParams a;
   int few;                               // requests of at most this many rows are not this kernel's
-  int32_t* tickets;                      // [2]: next item, CTAs that are done
   int32_t* status;
 };
 
@@ -58,9 +60,11 @@ struct Shared {
   alignas(16) uint8_t raw[2][128 * 16 * kSteps];                         // codes of a step's K and V on their way
   float4 scale[4][8];                    // per step (four in turn) and 16 keys: k_scale, log2 v_scale, 1 / v_scale
   Item item[2];
-  int items, last[2];
+  long long sums[kThreads / 32];
+  long long from, total, share[2];       // the CTA's share [share[0], share[1]) begins in request `request` (or behind it), which begins at `from`; the line's length
+  int request, last[2];
   alignas(8) uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2][2], p_full[2][2], pv_done[2][2], o_empty[2], item_full[2],
-      item_empty[2], ask, done[2];
+      item_empty[2], done[2];
   uint32_t tmem_base;
   volatile int abort;
 };
@@ -112,6 +116,21 @@ __device__ __forceinline__ int pairs_of(const ChunkParams& P, const Request& rq)
   return rows > P.few ? (rows + kPair - 1) / kPair : 0;
 }
 
+// tokens that the rows of a pair see at most, and its length on the line
+__device__ __forceinline__ int seen_of(const ChunkParams& P, const Request& rq, int rows_end) {
+  return max(min(min(rq.kv - rq.q_true + (rows_end - 1) / P.a.group + 1, rq.kv), P.a.max_kv), 0);
+}
+__device__ __forceinline__ int steps_of(const ChunkParams& P, const Request& rq, int pair) {
+  return max((seen_of(P, rq, min((pair + 1) * kPair, rq.q_len * P.a.group)) + kKeys - 1) / kKeys, 1);
+}
+__device__ __forceinline__ long long length_of(const ChunkParams& P, const Request& rq) {
+  long long n = 0;
+#pragma unroll 1
+  for (int i = pairs_of(P, rq); i > 0; --i) n += (long long)(steps_of(P, rq, i - 1) + kItemCost) * P.a.c.kv_heads;
+  return n;
+}
+__device__ __forceinline__ long long workers_of(long long total) { return max(min((long long)gridDim.x, total / kLeastShare), total > 0 ? 1ll : 0ll); }
+
 // place of 16-byte piece `c` (eight channels) of row `r` in a swizzled tile
 __device__ __forceinline__ uint32_t piece_at(int r, int c) {
   return uint32_t(c >> 3) * (128u * 128u) + uint32_t(r) * 128u + (uint32_t((c ^ r) & 7) << 4);
@@ -119,7 +138,7 @@ __device__ __forceinline__ uint32_t piece_at(int r, int c) {
 
 // A row's maximum rises (f = 2^(m - m'), 1 in rows that stay): `o_blocks` blocks of 16 accumulator columns of the warp's rows times f, once
 // the accumulator has the weights handed over so far.
-static __device__ __noinline__ bool bring_down(uint64_t& bar, uint32_t parity, volatile int* abort, int32_t* status, uint32_t t_o, int o_blocks, float f) {
+__device__ __forceinline__ bool bring_down(uint64_t& bar, uint32_t parity, volatile int* abort, int32_t* status, uint32_t t_o, int o_blocks, float f) {
   if (!__all_sync(0xffffffffu, wait_for(bar, parity, abort, 111, status))) return false;
   tc_fence_after();
 #pragma unroll 1
@@ -135,9 +154,14 @@ static __device__ __noinline__ bool bring_down(uint64_t& bar, uint32_t parity, v
   return true;
 }
 
-// A tile's part of an item that is cut along the keys: accumulators, m and Z of its rows (a row per thread).
+// A tile's part of an item that several CTAs share: accumulators, m and Z of its rows (a row per thread).  A CTA has room for two: of the item
+// that its share ends in, and of the one that it begins in.
 template <int kSteps>
-__device__ __noinline__ void put_part(float* part, int r, uint32_t t_o, bool any, float m, float z) {
+__device__ __forceinline__ float* part_of(const AttendParams& A, int w, int w0, int i) {
+  return A.partials + (int64_t(2 * w + (w == w0 ? 1 : 0)) * 2 + i) * (kTileRows * (16 * kSteps + 2));
+}
+template <int kSteps>
+__device__ __forceinline__ void put_part(float* part, int r, uint32_t t_o, bool any, float m, float z) {
   if (any) {
 #pragma unroll 1
     for (int b = 0; b < kSteps; ++b) {
@@ -156,14 +180,15 @@ __device__ __noinline__ void put_part(float* part, int r, uint32_t t_o, bool any
 // The output of a row: the accumulators, or parts joined in order.
 struct OutRow { int token, head; bool in; };
 template <int kSteps>
-__device__ __noinline__ float2 put_row(const AttendParams& A, OutRow row, int r, uint32_t t_o, bool any, float m, float z, const float* parts0, int parts) {
-  constexpr int dh = 16 * kSteps, kPart = kTileRows * (dh + 2);
+__device__ __forceinline__ float2 put_row(const AttendParams& A, OutRow row, int r, int i, uint32_t t_o, bool any, float m, float z, int w0, int parts) {
+  constexpr int dh = 16 * kSteps;
+  auto stats = [&](int p) { return __ldcg(reinterpret_cast<const float2*>(part_of<kSteps>(A, w0 + p, w0, i) + kTileRows * dh) + r); };
   if (parts > 1) {
     m = -CUDART_INF_F;
     z = 0.f;
-    for (int p = 0; p < parts; ++p) m = fmaxf(m, __ldcg(reinterpret_cast<const float2*>(parts0 + int64_t(2 * p) * kPart + kTileRows * dh) + r).x);
+    for (int p = 0; p < parts; ++p) m = fmaxf(m, stats(p).x);
     for (int p = 0; p < parts; ++p) {
-      const float2 mz = __ldcg(reinterpret_cast<const float2*>(parts0 + int64_t(2 * p) * kPart + kTileRows * dh) + r);
+      const float2 mz = stats(p);
       if (mz.x > -CUDART_INF_F) z = fmaf(ex2(mz.x - m), mz.y, z);
     }
   }
@@ -185,8 +210,8 @@ __device__ __noinline__ float2 put_row(const AttendParams& A, OutRow row, int r,
       for (int e = 0; e < 16; ++e) v[e] = 0.f;
 #pragma unroll 1
       for (int p = 0; p < parts; ++p) {
-        const float* pp = parts0 + int64_t(2 * p) * kPart;
-        const float mp = __ldcg(reinterpret_cast<const float2*>(pp + kTileRows * dh) + r).x;
+        const float* pp = part_of<kSteps>(A, w0 + p, w0, i);
+        const float mp = stats(p).x;
         if (mp == -CUDART_INF_F) continue;                // (saw nothing, wrote nothing)
         const float f = ex2(mp - m) * inv;
 #pragma unroll
@@ -227,7 +252,6 @@ template <int kSteps>
 __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_constant__ ChunkParams P) {
   using Sh = Shared<kSteps>;
   constexpr int dh = 16 * kSteps;
-  constexpr int kPart = kTileRows * (dh + 2);             // floats of a tile's part
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   Sh& S = *reinterpret_cast<Sh*>(smem_raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -249,7 +273,6 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
       mbar_init(smem_u32(&S.item_empty[i]), kSoftWarps + kConvWarps + 2);
       mbar_init(smem_u32(&S.done[i]), 1);
     }
-    mbar_init(smem_u32(&S.ask), 2);
     S.abort = 0;
     if (smem_u32(smem_raw) & 1023u) {
       atomicCAS(P.status, 0, 100);
@@ -269,21 +292,38 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
   grid_dependency_wait();
   grid_dependency_trigger();
 
-  // ---- items: row pairs of all requests, times heads
-  if (tid == 0) S.items = 0;
-  __syncthreads();
+  // ---- the line: requests in order, of one the row pairs from its end, of one the key / value heads
+  const int per = (P.a.requests + kThreads - 1) / kThreads, b_first = min(tid * per, P.a.requests), b_last = min(b_first + per, P.a.requests);
   {
-    int n = 0;
+    long long n = 0;
 #pragma unroll 1
-    for (int b = tid; b < P.a.requests; b += kThreads) n += pairs_of(P, request_of(P.a, b)) * P.a.c.kv_heads;
-    if (n > 0) atomicAdd(&S.items, n);
+    for (int b = b_first; b < b_last; ++b) n += length_of(P, request_of(P.a, b));
+    long long before = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long a = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += a;
+    }
+    if (lane == 31) S.sums[warp] = before;
+    __syncthreads();
+    long long total = 0;
+#pragma unroll 1
+    for (int w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) before += S.sums[w];
+      total += S.sums[w];
+    }
+    // the group of requests that the share begins in
+    const long long workers = workers_of(total), at = blockIdx.x < workers ? blockIdx.x * total / workers : total;
+    if (before - n <= at && at < before) { S.request = b_first; S.from = before - n; }
+    if (tid == 0) {
+      S.total = total;
+      S.share[0] = at;
+      S.share[1] = blockIdx.x < workers ? (blockIdx.x + 1) * total / workers : total;
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  const int items = S.items;
-  // parts of an item along the keys
-  const int parts = items > 0 && items <= int(gridDim.x) / 2 ? int(gridDim.x) / items : 1;
 
-  // What every role but the fetching warp does with an item: read it, hand the slot back.
+  // What conversion and MMA warps do with an item: read it, hand the slot back.
   auto next_item = [&](int it, Item& x) {
     if (!wait_for(S.item_full[it & 1], uint32_t(it >> 1), abort, 101, P.status)) { x.b = -1; }
     else x = S.item[it & 1];
@@ -296,67 +336,75 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
   if (warp >= kMmaWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == kItemWarp) {
-      // ---------------------------------------------------------------- items
-      // Level k holds the k-th row pair from the end of every request that has one, for every key / value head: the longest items come
-      // first.  The warp walks the levels along with its tickets.
-      auto pairs_in = [&](int b) { return b < P.a.requests ? pairs_of(P, request_of(P.a, b)) : 0; };
-      int level = -1, level_end = 0, level_start = 0;       // items up to the level's end, and before it
+      // ---------------------------------------------------------------- items (every lane walks the line alike)
+      const long long total = S.total, workers = workers_of(total);
+      const bool any = blockIdx.x < workers;
+      long long at = S.share[0], start = any ? S.from : 0;
+      const long long begin = at, end = S.share[1];
+      int b = any ? S.request : 0;
+      Request rq = {};
+      int pair = -1, each = 0;                            // of the request, and the length of one of its items
+      auto next_pair = [&]() {
+        --pair;
+        each = pair >= 0 ? steps_of(P, rq, pair) + kItemCost : 0;
+      };
+      if (any) {
+        rq = request_of(P.a, b);
+        pair = pairs_of(P, rq);
+        next_pair();
+      }
       for (int it = 0;; ++it) {
-        bool ok = it < 2 || wait_for(S.item_empty[it & 1], uint32_t((it >> 1) - 1), abort, 102, P.status);
-        // (taken when the item before it is two steps from its end, so that what is left goes to who is free)
-        ok = ok && (it == 0 || wait_for(S.ask, uint32_t(it - 1), abort, 113, P.status));
-        ok = __all_sync(0xffffffffu, ok);
-        int ticket = items * parts;
-        if (ok && lane == 0) ticket = atomicAdd(P.tickets, 1);
-        ticket = __shfl_sync(0xffffffffu, ticket, 0);
         Item x = {};
         x.b = -1;
-        if (ticket < items * parts) {
-          x.id = ticket / parts;
-          x.part = ticket - x.id * parts;
-          while (x.id >= level_end) {
-            ++level;
-            level_start = level_end;
-            for (int b = lane; b < P.a.requests + lane; b += 32)               // (all lanes the same number of times)
-              level_end += __popc(__ballot_sync(0xffffffffu, pairs_in(b) > level)) * P.a.c.kv_heads;
+        while (at < end) {
+          const long long group = (long long)each * P.a.c.kv_heads;          // the pair's items (none left: 0)
+          if (at >= start + group) {
+            start += group;
+            if (pair < 0) {
+              rq = request_of(P.a, ++b);
+              pair = pairs_of(P, rq);
+            }
+            next_pair();
+            continue;
           }
-          int nth = (x.id - level_start) / P.a.c.kv_heads, b0 = 0;
-          x.h = x.id - level_start - nth * P.a.c.kv_heads;
-          uint32_t have = __ballot_sync(0xffffffffu, pairs_in(lane) > level);
-          while (nth >= __popc(have)) {
-            nth -= __popc(have);
-            b0 += 32;
-            have = __ballot_sync(0xffffffffu, pairs_in(b0 + lane) > level);
-          }
-          for (; nth > 0; --nth) have &= have - 1;
-          x.b = b0 + __ffs(have) - 1;
-          const Request rq = request_of(P.a, x.b);
-          x.row0 = (pairs_of(P, rq) - 1 - level) * kPair;
+          x.h = int(uint32_t(at - start) / uint32_t(each));
+          const long long item_at = start + (long long)x.h * each;
+          const int o0 = int(at - item_at), o1 = int(min((long long)each, o0 + (end - at)));
+          at += o1 - o0;
+          if (o1 <= kItemCost) continue;                  // (none of its steps)
+          x.b = b;
+          x.row0 = pair * kPair;
           x.q0 = rq.q0;
           x.before = rq.kv - rq.q_true;
           x.n_rows = rq.q_len * P.a.group;
-          int seen[2];
+          x.j0 = max(o0 - kItemCost, 0);
+          const int j1 = o1 - kItemCost;
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const int rows = min(x.n_rows - x.row0 - i * kTileRows, kTileRows);
-            seen[i] = rows > 0 ? max(min(min(x.before + (x.row0 + i * kTileRows + rows - 1) / P.a.group + 1, rq.kv), P.a.max_kv), 0) : 0;
+            const int rows_end = min(x.row0 + (i + 1) * kTileRows, x.n_rows);
+            const int seen = rows_end > x.row0 + i * kTileRows ? seen_of(P, rq, rows_end) : 0;
+            x.ends[i] = max(min((seen + kHalf - 1) / kHalf, 2 * j1) - 2 * x.j0, 0);
           }
-          const int most = (max(seen[0], seen[1]) + kKeys - 1) / kKeys;
-          x.j0 = int((long long)most * x.part / parts);
-          const int j1 = int((long long)most * (x.part + 1) / parts);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) x.ends[i] = max(min((seen[i] + kHalf - 1) / kHalf, 2 * j1) - 2 * x.j0, 0);
+          // the shares that hold its first step and its last
+          // (share w begins at floor(w total / workers), so it begins at or before position p if w total < (p + 1) workers)
+          int w0 = int(blockIdx.x), w1 = w0;
+          if (item_at + kItemCost < begin)
+            while (w0 * total >= (item_at + kItemCost + 1) * workers) --w0;
+          if (item_at + each > end)
+            while ((w1 + 1) * total < (item_at + each) * workers) ++w1;
+          x.w0 = w0;
+          x.parts = w1 - w0 + 1;
+          break;
         }
+        bool ok = it < 2 || wait_for(S.item_empty[it & 1], uint32_t((it >> 1) - 1), abort, 102, P.status);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) x.b = -1;
         if (lane == 0) {
           S.item[it & 1] = x;
           mbar_arrive(smem_u32(&S.item_full[it & 1]));
         }
         __syncwarp();
         if (x.b < 0) break;
-      }
-      if (lane == 0 && atomicAdd(P.tickets + 1, 1) == int(gridDim.x) - 1) {     // the counters for the next call
-        P.tickets[0] = 0;
-        P.tickets[1] = 0;
       }
     } else if (warp < kItemWarp) {
       // ---------------------------------------------------------------- MMAs of tile i
@@ -414,7 +462,6 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
       for (int it = 0; ok && next_item(it, x); ++it) {
         const int end = __shfl_sync(0xffffffffu, x.ends[i], 0), other = __shfl_sync(0xffffffffu, x.ends[i ^ 1], 0);    // steps of 64 keys
         const int n = (max(end, other) + 1) >> 1;         // steps of 128
-        if (n <= 3 && lane == 0) mbar_arrive(smem_u32(&S.ask));
         if (n <= 0) continue;
         if (!await(S.k_full[g & 1], g >> 1, 103)) break;
         if (end > 0) {
@@ -425,7 +472,6 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
         release(S.k_empty[g & 1]);
 #pragma unroll 1
         for (int j = 0; j < n; ++j) {
-          if (j + 3 == n && lane == 0) mbar_arrive(smem_u32(&S.ask));
           const uint32_t at = g + uint32_t(j), next = at + 1;
           const int left = end - 2 * j;                   // of the tile's steps
           if (!await(S.v_full[at & 1], at >> 1, 106)) break;
@@ -692,21 +738,21 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
 
       // ---- the row
       bool writes = true;
-      const float* parts0 = A.partials + (int64_t(x.id) * parts * 2 + i) * kPart;
+      const int parts = x.parts, w0 = x.w0;
       if (parts > 1) {
-        put_part<kSteps>(const_cast<float*>(parts0) + int64_t(2 * x.part) * kPart, r, t_o, n > 0, m, z);
+        put_part<kSteps>(part_of<kSteps>(A, int(blockIdx.x), w0, i), r, t_o, n > 0, m, z);
         tile_barrier();
         if (r == 0) {
-          const int seen = atomicAdd(A.counters + 2 * x.id + i, 1);
+          const int seen = atomicAdd(A.counters + 2 * w0 + i, 1);
           S.last[i] = seen == parts - 1;
-          if (seen == parts - 1) A.counters[2 * x.id + i] = 0;
+          if (seen == parts - 1) A.counters[2 * w0 + i] = 0;                 // (nobody else counts here any more)
         }
         tile_barrier();
         writes = S.last[i] != 0;
         if (writes) __threadfence();
       }
       if (writes) {
-        const float2 mz = put_row<kSteps>(A, row, r, t_o, n > 0, m, z, parts0, parts);
+        const float2 mz = put_row<kSteps>(A, row, r, i, t_o, n > 0, m, z, w0, parts);
         if (row.in && A.lse)
           A.lse[int64_t(row.token) * A.heads + row.head] = mz.y > 0.f ? (mz.x - kLift + log2f(mz.y)) * kLn2 : mz.y == 0.f ? -CUDART_INF_F : CUDART_NAN_F;
       }
@@ -739,8 +785,7 @@ repq_status launch(const AttendParams& A, const ChunksPlan& plan, int few, void*
   ChunkParams P;
   P.a = A;
   P.few = few;
-  P.tickets = static_cast<int32_t*>(workspace);
-  P.a.counters = P.tickets + 2;
+  P.a.counters = static_cast<int32_t*>(workspace);
   P.a.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + plan.counter_bytes);
   P.status = device_status_word();
   REPQ_REQUIRE(P.status != nullptr, REPQ_CUDA_ERROR, "repq_cache_attention: no device status word");

@@ -288,9 +288,10 @@ __device__ __forceinline__ Share share_of(const AttendParams& P, const Request& 
 }
 
 // A job costs a share as much as so many units beside its own: its queries, the join of its warps, its output.  Where lengths differ, shares of
-// many short jobs would otherwise be the last to end (64 requests of 1 to 4096 tokens: 84 us without, ... with).  Calls of few units deal
+// many short jobs would otherwise be the last to end (64 requests of 1 to 4096 tokens: 84 us without, 67 with 2,
+// 59 with 4 or 6).  Calls of few units deal
 // out bare units.
-constexpr int kJobCost = 2;
+constexpr int kJobCost = 4;
 
 template <int kSteps, int kTiles, bool kPrecise>
 __global__ void __launch_bounds__(kThreads, kTiles == 1 && !kPrecise && kSteps < 7 ? 4 : 3) cache_rows_kernel(const __grid_constant__ AttendParams P) {
