@@ -1,0 +1,204 @@
+"""Serving a quantized decoder: blocks that keep keys and values in a paged 8-bit cache, and log probabilities of tokens.
+
+A step brings some tokens of some requests (prompts, chunks of prompts, single tokens, all in one batch).  `PagedCache.plan` finds
+blocks and slots for them on the GPU, `CachedBlock.forward_cached` runs a block over the step's tokens, and `Decoder` chains blocks, the
+final normalisation and the vocabulary projection.  As in `engine`, this module prepares once and then only sequences library
+calls; everything is queued on the current stream, and lengths are known on the host too (a program knows what it asked for), so nothing is
+read back."""
+from __future__ import annotations
+
+import dataclasses
+from typing import List, Optional, Sequence
+
+import numpy as np
+import torch
+
+from . import binding as B
+from .engine import PreparedLinear, QuantBlock, _pack_linear
+
+
+@dataclasses.dataclass
+class Step:
+    """What the tokens of one step share: tensors on the device, sizes on the host."""
+    cu_q: torch.Tensor          # int32 [requests + 1]
+    kv_lens: torch.Tensor       # int32 [requests], this step's tokens included
+    slot_map: torch.Tensor      # int32 [tokens]
+    positions: torch.Tensor     # int32 [tokens]
+    last_rows: torch.Tensor     # int64: the last row of every request that brings tokens
+    tokens: int
+    max_q_len: int
+    max_kv_len: int
+
+
+class PagedCache:
+    """Keys and values of up to `requests` requests for every layer of a decoder, in blocks dealt out of one pool."""
+
+    def __init__(self, layers: int, num_blocks: int, kv_heads: int, block_size: int, d_h: int, requests: int,
+                 max_tokens: int, device="cuda:0"):
+        dev = torch.device(device)
+        self.layers = [B.new_cache(num_blocks, kv_heads, block_size, d_h, dev) for _ in range(layers)]
+        self.block_size, self.requests, self.max_tokens, self.device = block_size, requests, max_tokens, dev
+        ints = lambda *s: torch.zeros(*s, dtype=torch.int32, device=dev)                    # noqa: E731
+        self.table = torch.full((requests, -(-max_tokens // block_size)), -1, dtype=torch.int32, device=dev)
+        self.free_list = torch.arange(num_blocks, dtype=torch.int32, device=dev)
+        # (the plan reads one pair and writes the other)
+        self._kv, self._head = [ints(requests), ints(requests)], [ints(1), ints(1)]
+        self._turn = 0
+        self.lens = [0] * requests                     # the same on the host
+        self.free_blocks = num_blocks
+        self._workspace: Optional[torch.Tensor] = None
+
+    def _blocks(self, tokens: int) -> int:
+        return -(-tokens // self.block_size)
+
+    def plan(self, q_lens: Sequence[int]) -> Step:
+        """Room for q_lens[b] more tokens of every request; raises, and changes nothing, where there is none."""
+        if len(q_lens) != self.requests or min(q_lens, default=0) < 0:
+            raise ValueError("plan: a number of tokens, 0 or more, for every one of %d requests" % self.requests)
+        lens = [a + int(b) for a, b in zip(self.lens, q_lens)]
+        if max(lens, default=0) > self.max_tokens:
+            raise ValueError("plan: a request would hold more than %d tokens" % self.max_tokens)
+        need = sum(self._blocks(b) - self._blocks(a) for a, b in zip(self.lens, lens))
+        if need > self.free_blocks:
+            raise MemoryError("plan: %d blocks are needed and %d are free" % (need, self.free_blocks))
+        total, n, dev = int(sum(q_lens)), self.requests, self.device
+        new = lambda m: torch.empty(m, dtype=torch.int32, device=dev)                       # noqa: E731
+        q = torch.tensor(list(q_lens), dtype=torch.int32).to(dev)
+        cu, slots, pos = new(n + 1), new(total), new(total)
+        t = self._turn
+        B.repq_cache_plan(self._kv[t], q, self.table, self.free_list, self._head[t], self.block_size, kv_lens_out=self._kv[1 - t],
+                          cu_q=cu, slot_map=slots, positions=pos, free_head_out=self._head[1 - t])
+        ends = np.cumsum(np.asarray(q_lens, dtype=np.int64))
+        last = torch.from_numpy(ends[np.asarray(q_lens) > 0] - 1).to(dev)
+        self._turn, self.lens, self.free_blocks = 1 - t, lens, self.free_blocks - need
+        # (the step has lengths of its own: the next plan writes the pair anew)
+        return Step(cu, self._kv[1 - t].clone(), slots, pos, last, total, int(max(q_lens, default=0)), max(lens, default=0))
+
+    def release(self, request: int) -> None:
+        """The request's blocks go back to the free list."""
+        n, t = self._blocks(self.lens[request]), self._turn
+        if n:
+            head = self.free_list.numel() - self.free_blocks
+            self.free_list[head - n:head] = self.table[request, :n]
+            self._head[t].sub_(n)
+        self._kv[t][request] = 0
+        self.lens[request], self.free_blocks = 0, self.free_blocks + n
+
+    def workspace(self, nbytes: int) -> torch.Tensor:
+        """Zero-filled scratch of repq_cache_attention, which every call leaves ready for the next."""
+        if self._workspace is None or self._workspace.numel() < nbytes:
+            self._workspace = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+        return self._workspace
+
+
+class CachedBlock(QuantBlock):
+    """A block in its serving form: queries stay in bf16, keys and values go to the cache in 8 bits (a scale per block of tokens and
+    head in place of the block's one), probabilities are not quantized; the LayerNorms, the four linear layers and the quantizers in front of
+    them are those of QuantBlock."""
+
+    def _gemm(self, rows, a, s, z, row_sum, lin: PreparedLinear, n, k, out, **kw) -> None:
+        ab = self.cfg["bits_a"] | B.REPQ_BYTE_CODES
+        d = B.gemm_desc(rows, n, k, a, ab, s, z, lin.codes, self.bits_w, out, s_w=lin.s_w, z_w=lin.z_w, w_row_sum=lin.w_row_sum,
+                        bias=lin.bias, a_row_sum=row_sum, **kw)
+        ws = torch.empty(max(B.repq_qgemm_workspace_bytes(d), 16), dtype=torch.uint8, device=self.device)
+        B.repq_qgemm(d, ws)
+
+    def forward_cached(self, x: torch.Tensor, step: Step, cache: PagedCache, layer: int, y: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """x: [tokens of the step, dim] in the activation dtype.  The step's keys and values are written to `cache`'s layer first, so
+        its tokens see each other as well as what the cache held."""
+        c = self.cfg
+        D, H, mlp, T = c["D"], c["H"], c["MLP"], step.tokens
+        dh, dev = D // H, x.device
+        if x.dtype != self.act_dtype or x.shape != (T, D) or not x.is_contiguous():
+            raise ValueError("forward_cached: x is [tokens of the step, dim], dense, in the activation dtype")
+        if not c["causal"]:
+            raise ValueError("forward_cached: the block attends in both directions; a cache holds causal ones")
+        if self.rope is not None and step.max_kv_len > c["L"]:
+            raise ValueError("forward_cached: the rotation table ends at position %d" % c["L"])
+        if y is None:
+            y = torch.empty((T, D), dtype=self.out_dtype, device=dev)
+        if T == 0:
+            return y
+        ab = c["bits_a"] | B.REPQ_BYTE_CODES
+        norm = B.REPQ_NORM_RMS if self.llama else B.REPQ_NORM_LAYERNORM
+        kind = lambda t: B.REPQ_OUT_F32 if t.dtype == torch.float32 else B.REPQ_OUT_BF16     # noqa: E731
+        codes, sums = torch.empty(T, D, dtype=torch.uint8, device=dev), torch.empty(T, dtype=torch.int32, device=dev)
+        B.repq_ln_quant(x, self.ln1_g, self.ln1_b, c["eps"], self.ln1_s, self.ln1_z, ab, codes, sums, norm)
+        qkv = torch.empty(T, 3 * D, dtype=self.act_dtype, device=dev)
+        kw = dict(out_scale=[1.0] * 3, out_zero=[0] * 3, out_kind=kind(qkv))
+        if self.rope is not None:                       # a row of the table per token: the positions of a step are not those of its rows
+            kw.update(rope=self.rope.index_select(0, step.positions), rope_period=T, rope_dim=dh, rope_groups=2)
+        self._gemm(T, codes, self.ln1_s, self.ln1_z, sums, self.qkv, 3 * D, D, qkv, **kw)
+        q, k, v = (qkv.view(T, 3 * H, dh)[:, i * H:(i + 1) * H] for i in range(3))
+        tensors = cache.layers[layer]
+        B.repq_cache_write(tensors, k, v, step.slot_map)
+        ws = cache.workspace(B.repq_cache_attention_workspace_bytes(tensors, q, cache.table, step.max_q_len, step.max_kv_len))
+        s_at, z_at = self.act_q["attn"]
+        sums.zero_()
+        B.repq_cache_attention(tensors, q, cache.table, step.kv_lens, step.cu_q, codes.view(T, H, dh), ws, max_q_len=step.max_q_len,
+                               max_kv_len=step.max_kv_len, alpha=1.0 / float(np.sqrt(dh)), out_bits=ab, out_scale=s_at, out_zero=z_at,
+                               out_row_sum=sums)
+        xbar = torch.empty(T, D, dtype=self.act_dtype, device=dev)
+        self._gemm(T, codes, s_at, z_at, sums, self.proj, D, D, xbar, residual=x, out_kind=kind(xbar))
+        codes2, sums2, sums3 = torch.empty_like(codes), torch.empty_like(sums), torch.zeros_like(sums)
+        B.repq_ln_quant(xbar, self.ln2_g, self.ln2_b, c["eps"], self.ln2_s, self.ln2_z, ab, codes2, sums2, norm)
+        hidden = torch.empty(T, mlp, dtype=torch.uint8, device=dev)
+        s_h, z_h = self.act_q["hidden"]
+        self._gemm(T, codes2, self.ln2_s, self.ln2_z, sums2, self.fc1, 2 * mlp if self.llama else mlp, D, hidden, gelu=not self.llama,
+                   glu=self.llama, out_kind=B.REPQ_OUT_CODES, out_bits=ab, out_scale=[s_h], out_zero=[z_h], out_row_sum=sums3)
+        self._gemm(T, hidden, s_h, z_h, sums3, self.fc2, D, mlp, y, residual=xbar, out_kind=kind(y))
+        return y
+
+
+@dataclasses.dataclass
+class Scores:
+    """Log probabilities of given tokens, the rows' entropy (nats), the tokens' rank and the most probable alternatives."""
+    logprob: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    rank: Optional[torch.Tensor]
+    top_ids: torch.Tensor
+    top_logprobs: torch.Tensor
+
+
+def score(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 1) -> Scores:
+    """repq_token_logprobs into new tensors; logits [rows, vocab], tokens int32 [rows] or None."""
+    n, dev = logits.shape[0], logits.device
+    f = lambda *s: torch.empty(*s, dtype=torch.float32, device=dev)                          # noqa: E731
+    i = lambda *s: torch.empty(*s, dtype=torch.int32, device=dev)                            # noqa: E731
+    out = Scores(f(n) if tokens is not None else None, f(n), i(n) if tokens is not None else None, i(n, top), f(n, top))
+    B.repq_token_logprobs(logits, tokens, out.logprob, entropy=out.entropy, rank=out.rank, top_ids=out.top_ids if top else None,
+                          top_logprobs=out.top_logprobs if top else None)
+    return out
+
+
+class Decoder:
+    """Blocks, final normalisation and vocabulary projection of a decoder, in serving form."""
+
+    def __init__(self, blocks: List[CachedBlock], embedding: torch.Tensor, norm_gamma: np.ndarray, norm_beta: np.ndarray, norm_lo: np.ndarray,
+                 norm_hi: np.ndarray, w_head: np.ndarray):
+        """embedding: [vocab, dim] on the device in the activation dtype; the norm_* arrays are the final normalisation's affine factors and
+        the clipping bounds of its output, per channel; w_head: [vocab, dim]."""
+        b = blocks[0]
+        self.blocks, self.embedding, self.vocab = blocks, embedding, w_head.shape[0]
+        s, z = B.repq_scale_zero_from_bounds(norm_lo, norm_hi, b.cfg["bits_a"])
+        g, beta, self.s, self.z, w, bias = B.repq_fold_ln(norm_gamma, norm_beta, s, z, w_head, np.zeros(self.vocab, dtype=np.float32))
+        self.gamma, self.beta = torch.from_numpy(g).to(b.device), torch.from_numpy(beta).to(b.device)
+        self.head = _pack_linear(w, bias, b.bits_w, b.device)
+
+    def forward(self, tokens: torch.Tensor, step: Step, cache: PagedCache, rows: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Float32 logits of the step's tokens (int32 or int64 [tokens]), or of the given rows of them (step.last_rows to go on
+        from)."""
+        b = self.blocks[0]
+        x = self.embedding.index_select(0, tokens)
+        for layer, block in enumerate(self.blocks):
+            x = block.forward_cached(x, step, cache, layer)
+        if rows is not None:
+            x = x.index_select(0, rows)
+        T, D = x.shape
+        logits = torch.empty(T, self.vocab, dtype=torch.float32, device=x.device)
+        if T:
+            codes, sums = torch.empty(T, D, dtype=torch.uint8, device=x.device), torch.empty(T, dtype=torch.int32, device=x.device)
+            B.repq_ln_quant(x, self.gamma, self.beta, b.cfg["eps"], self.s, self.z, b.cfg["bits_a"] | B.REPQ_BYTE_CODES, codes, sums,
+                            B.REPQ_NORM_RMS if b.llama else B.REPQ_NORM_LAYERNORM)
+            b._gemm(T, codes, self.s, self.z, sums, self.head, self.vocab, D, logits)
+        return logits
