@@ -30,7 +30,7 @@ repq_status prepare(const repq_cache_attention_desc* d, AttendParams* out, bool*
   P.scale = d->alpha * 1.4426950408889634f;
   P.out_kind = d->out_kind;
   P.out = d->out; P.ldo = d->ldo; P.o_sh = d->o_stride_head;
-  P.out_wide = aligned(d->out, 32) && (d->ldo | d->o_stride_head) * (d->out_kind == REPQ_OUT_F32 ? 4 : 2) % 32 == 0;
+  P.out_wide = aligned(d->out, 16) && (d->ldo | d->o_stride_head) * (d->out_kind == REPQ_OUT_F32 ? 4 : d->out_kind == REPQ_OUT_BF16 ? 2 : 1) % 16 == 0;
   P.out_row_sum = nullptr;
   P.lse = d->lse;
   if (d->out_kind == REPQ_OUT_CODES) {

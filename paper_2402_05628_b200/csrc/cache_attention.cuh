@@ -23,7 +23,7 @@ struct AttendParams {
   int out_kind, qmax, pack4;
   float inv_so; int zo;
   void* out; int64_t ldo, o_sh;
-  int out_wide;                          // output rows are 32-byte aligned
+  int out_wide;                          // output rows are 16-byte aligned
   int32_t* out_row_sum;
   float* lse;
   int32_t* counters;                     // workspace: one per worker, zero between calls
@@ -64,6 +64,11 @@ __device__ __forceinline__ Request request_of(const AttendParams& P, int b) {
   return r;
 }
 
+__device__ __forceinline__ int2 code_pair(const AttendParams& P, float a, float b) {
+  const float lo = float(-P.zo), hi = float(P.qmax - P.zo);
+  return make_int2(__float2int_rn(fminf(fmaxf(a * P.inv_so, lo), hi)) + P.zo, __float2int_rn(fminf(fmaxf(b * P.inv_so, lo), hi)) + P.zo);
+}
+
 // Two neighbouring channels of an output row; the codes' sum for the row sums.
 __device__ __forceinline__ int store_pair(const AttendParams& P, int token, int head, int d, float a, float b) {
   const int64_t at = token * P.ldo + head * P.o_sh;
@@ -75,8 +80,8 @@ __device__ __forceinline__ int store_pair(const AttendParams& P, int token, int 
     *reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(P.out) + at + d) = __floats2bfloat162_rn(a, b);
     return 0;
   }
-  const float lo = float(-P.zo), hi = float(P.qmax - P.zo);
-  const int ca = __float2int_rn(fminf(fmaxf(a * P.inv_so, lo), hi)) + P.zo, cb = __float2int_rn(fminf(fmaxf(b * P.inv_so, lo), hi)) + P.zo;
+  const int2 k = code_pair(P, a, b);
+  const int ca = k.x, cb = k.y;
   uint8_t* o = static_cast<uint8_t*>(P.out) + at;
   if (P.pack4) o[d >> 1] = uint8_t(ca | cb << 4);
   else *reinterpret_cast<uint16_t*>(o + d) = uint16_t(ca | cb << 8);

@@ -33,8 +33,8 @@ constexpr int kKeys = 128, kHalf = 64;   // keys that are converted at a time, a
 constexpr int kSoftWarps = 8, kConvWarps = 4;
 constexpr int kMmaWarp = kSoftWarps + kConvWarps, kItemWarp = kMmaWarp + 2;       // (an MMA warp per tile)
 constexpr int kThreads = 512;             // (the last warp has nothing to do)
-// Registers per thread, dealt out anew once the roles part: 256 x 176 + 128 x 80 + 128 x 80 = the 512 x 128 of the launch
-constexpr int kSoftRegs = 176, kConvRegs = 80, kOtherRegs = 80;
+// Registers per thread, dealt out anew once the roles part: 256 x 168 + 128 x 112 + 128 x 64 = the 512 x 128 of the launch
+constexpr int kSoftRegs = 168, kConvRegs = 112, kOtherRegs = 64;
 constexpr float kLift = 7.f, kLag = 8.f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -57,7 +57,7 @@ struct Shared {
   alignas(1024) uint8_t q[2][kTile];
   alignas(1024) uint8_t k[2][kTile];
   alignas(1024) uint8_t v[2][kTile];
-  alignas(16) uint8_t raw[2][128 * 16 * kSteps];                         // codes of a step's K and V on their way
+  alignas(16) uint8_t stage[kSoftWarps][32 * 128];                       // outputs on their way
   float4 scale[4][8];                    // per step (four in turn) and 16 keys: k_scale, log2 v_scale, 1 / v_scale
   Item item[2];
   long long sums[kThreads / 32];
@@ -177,76 +177,140 @@ __device__ __forceinline__ void put_part(float* part, int r, uint32_t t_o, bool 
   __threadfence();
 }
 
-// The output of a row: the accumulators, or parts joined in order.
-struct OutRow { int token, head; bool in; };
+// Parts joined in order, into the accumulators: m and Z of the row.  (A part that saw nothing has written nothing but that.)
 template <int kSteps>
-__device__ __forceinline__ float2 put_row(const AttendParams& A, OutRow row, int r, int i, uint32_t t_o, bool any, float m, float z, int w0, int parts) {
-  constexpr int dh = 16 * kSteps;
-  auto stats = [&](int p) { return __ldcg(reinterpret_cast<const float2*>(part_of<kSteps>(A, w0 + p, w0, i) + kTileRows * dh) + r); };
-  if (parts > 1) {
-    m = -CUDART_INF_F;
-    z = 0.f;
-    for (int p = 0; p < parts; ++p) m = fmaxf(m, stats(p).x);
+__device__ __forceinline__ float2 join_parts(const AttendParams& A, int r, int i, uint32_t t_o, int w0, int parts) {
+  constexpr int kCols = kSteps % 2 ? 16 : 32;             // at a time: the loads of two parts are on their way together
+  auto stats = [&](int p) { return __ldcg(reinterpret_cast<const float2*>(part_of<kSteps>(A, w0 + p, w0, i) + kTileRows * 16 * kSteps) + r); };
+  float m = -CUDART_INF_F, z = 0.f;
+#pragma unroll 2
+  for (int p = 0; p < parts; ++p) {
+    const float2 mz = stats(p);
+    const float up = fmaxf(m, mz.x), base = up == -CUDART_INF_F ? 0.f : up;
+    z = z * ex2(m - base) + ex2(mz.x - base) * mz.y;      // (2^-inf = 0)
+    m = up;
+  }
+  const float base = m == -CUDART_INF_F ? 0.f : m;
+#pragma unroll 1
+  for (int c = 0; c < 16 * kSteps; c += kCols) {
+    float v[kCols];
+#pragma unroll
+    for (int e = 0; e < kCols; ++e) v[e] = 0.f;
+#pragma unroll 2
     for (int p = 0; p < parts; ++p) {
-      const float2 mz = stats(p);
-      if (mz.x > -CUDART_INF_F) z = fmaf(ex2(mz.x - m), mz.y, z);
+      const float mp = stats(p).x;
+      const float4* from = reinterpret_cast<const float4*>(part_of<kSteps>(A, w0 + p, w0, i)) + (c >> 2) * kTileRows + r;
+      float4 w[kCols / 4];
+#pragma unroll
+      for (int e = 0; e < kCols / 4; ++e) w[e] = __ldcg(from + e * kTileRows);
+      const bool saw = mp > -CUDART_INF_F;
+      const float f = ex2(mp - base);
+#pragma unroll
+      for (int e = 0; e < kCols / 4; ++e) {
+        v[4 * e] = fmaf(f, saw ? w[e].x : 0.f, v[4 * e]);
+        v[4 * e + 1] = fmaf(f, saw ? w[e].y : 0.f, v[4 * e + 1]);
+        v[4 * e + 2] = fmaf(f, saw ? w[e].z : 0.f, v[4 * e + 2]);
+        v[4 * e + 3] = fmaf(f, saw ? w[e].w : 0.f, v[4 * e + 3]);
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < kCols / 16; ++h) {
+      uint32_t w[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(v[16 * h + e]);
+      tmem_st16(t_o + uint32_t(c + 16 * h), w);
     }
   }
-  const float inv = z > 0.f ? __fdividef(1.f, z) : z == 0.f ? 0.f : CUDART_NAN_F;
-  int sum = 0;
+  tmem_st_wait();
+  return make_float2(m, z);
+}
+
+// The output of a warp's 32 rows: accumulators times `inv` of their row.  A thread forms pieces of its row, which pass through 4 KB of shared
+// memory, 128 bytes of every row at a time, so that a store of the warp touches four lines and not 32 (rows stored by their threads: 4700
+// to 7400 cycles an item, up to two steps of both tiles).  off: where the thread's row begins in the output, -1 for rows that are none.
+template <int kSteps>
+__device__ __forceinline__ void put_rows(const AttendParams& A, uint8_t* stage, int64_t off, int token, uint32_t t_o, bool any, float inv, int lane) {
+  const int kind = A.out_kind, lg = kind == REPQ_OUT_F32 ? 2 : kind == REPQ_OUT_BF16 ? 1 : 0;
+  const int row_bytes = A.pack4 ? 8 * kSteps : (16 * kSteps) << lg;
+  off <<= lg;
+  const bool whole = A.out_wide && row_bytes % 16 == 0;   // (in pieces of 16 bytes)
+  int64_t rows[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) rows[k] = __shfl_sync(0xffffffffu, off, 4 * k + (lane >> 3));
+  int sum = 0, piece = 0, from = 0;                       // the next piece of the stage, and where its first one lies in the rows
+  uint8_t* mine = stage + 128 * lane;
+  auto put = [&](uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    *reinterpret_cast<uint4*>(mine + (((piece ^ lane) & 7) << 4)) = make_uint4(x, y, z, w);
+    ++piece;
+  };
 #pragma unroll 1
-  for (int b = 0; b < kSteps; ++b) {
-    float v[16];
-    if (parts == 1) {
-      uint32_t w[16] = {};
-      if (any) {
-        tmem_ld16(t_o + 16u * b, w);
-        tmem_ld_wait(w);
+  for (int c = 0; c < 16 * kSteps; c += 32) {
+    uint32_t w[32];                                       // (columns past the head hold anything)
+    tmem_ld32(t_o + uint32_t(c), w);
+    tmem_ld_wait32(w);
+#pragma unroll
+    for (int e = 0; e < 32; ++e) w[e] = any ? __float_as_uint(__uint_as_float(w[e]) * inv) : 0u;
+    if (kind == REPQ_OUT_BF16) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(w[2 * e]), __uint_as_float(w[2 * e + 1]));
+        w[e] = *reinterpret_cast<const uint32_t*>(&h);
       }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(w[e]) * inv;
+      for (int e = 0; e < 16; e += 4) put(w[e], w[e + 1], w[e + 2], w[e + 3]);
+    } else if (kind == REPQ_OUT_F32) {
+#pragma unroll
+      for (int e = 0; e < 32; e += 4) put(w[e], w[e + 1], w[e + 2], w[e + 3]);
     } else {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) v[e] = 0.f;
-#pragma unroll 1
-      for (int p = 0; p < parts; ++p) {
-        const float* pp = part_of<kSteps>(A, w0 + p, w0, i);
-        const float mp = stats(p).x;
-        if (mp == -CUDART_INF_F) continue;                // (saw nothing, wrote nothing)
-        const float f = ex2(mp - m) * inv;
+      for (int e = 0; e < 16; ++e) {
+        const int2 k = code_pair(A, __uint_as_float(w[2 * e]), __uint_as_float(w[2 * e + 1]));
+        if (c + 2 * e < 16 * kSteps) sum += k.x + k.y;
+        w[e] = uint32_t(A.pack4 ? k.x | k.y << 4 : k.x | k.y << 8);
+      }
+      if (A.pack4) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float4 w = __ldcg(reinterpret_cast<const float4*>(pp) + (4 * b + e) * kTileRows + r);
-          v[4 * e] = fmaf(f, w.x, v[4 * e]);
-          v[4 * e + 1] = fmaf(f, w.y, v[4 * e + 1]);
-          v[4 * e + 2] = fmaf(f, w.z, v[4 * e + 2]);
-          v[4 * e + 3] = fmaf(f, w.w, v[4 * e + 3]);
+        for (int e = 0; e < 4; ++e) w[e] = w[4 * e] | w[4 * e + 1] << 8 | w[4 * e + 2] << 16 | w[4 * e + 3] << 24;
+        put(w[0], w[1], w[2], w[3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = w[2 * e] | w[2 * e + 1] << 16;
+        put(w[0], w[1], w[2], w[3]);
+        put(w[4], w[5], w[6], w[7]);
+      }
+    }
+    if (piece < 8 && c + 32 < 16 * kSteps) continue;
+    __syncwarp();
+    const int p = lane & 7, at = from + 16 * p, left = p < piece ? row_bytes - at : 0;
+    const uint8_t* here = stage + 128 * (lane >> 3);
+#pragma unroll
+    for (int k0 = 0; k0 < 8; k0 += 4) {
+      uint4 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const uint4*>(here + 512 * (k0 + k) + (((p ^ (4 * k + (lane >> 3))) & 7) << 4));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint8_t* to = static_cast<uint8_t*>(A.out) + rows[k0 + k] + at;
+        if (rows[k0 + k] < 0 || left <= 0) continue;
+        if (whole) {
+          *reinterpret_cast<uint4*>(to) = v[k];
+        } else {                                          // codes: rows are whole words
+          uint32_t* to4 = reinterpret_cast<uint32_t*>(to);
+          to4[0] = v[k].x;
+          if (left > 4) to4[1] = v[k].y;
+          if (left > 8) to4[2] = v[k].z;
+          if (left > 12) to4[3] = v[k].w;
         }
       }
     }
-    if (row.in && A.out_kind == REPQ_OUT_BF16) {
-      uint32_t w[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
-        w[e] = *reinterpret_cast<const uint32_t*>(&h);
-      }
-      __nv_bfloat16* o = static_cast<__nv_bfloat16*>(A.out) + row.token * A.ldo + row.head * A.o_sh + 16 * b;
-      if (A.out_wide) {                                   // (half the passes of a store that touches 32 rows)
-        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                     ::"l"(o), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
-      } else {
-        reinterpret_cast<uint4*>(o)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        reinterpret_cast<uint4*>(o)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-      }
-    } else if (row.in) {
-#pragma unroll 1
-      for (int e = 0; e < 8; ++e) sum += store_pair(A, row.token, row.head, 16 * b + 2 * e, v[2 * e], v[2 * e + 1]);
-    }
+    __syncwarp();
+    from += 128;
+    piece = 0;
   }
-  if (row.in && A.out_row_sum) atomicAdd(A.out_row_sum + row.token, sum);
-  return make_float2(m, z);
+  if (off >= 0 && A.out_row_sum) atomicAdd(A.out_row_sum + token, sum);
 }
+
+struct OutRow { int token, head; bool in; };
 
 template <int kSteps>
 __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_constant__ ChunkParams P) {
@@ -505,6 +569,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
     constexpr int kPer = kSteps;                          // pieces of 16 codes of a thread: 128 rows x kSteps over 128 threads
     const AttendParams& A = P.a;
     uint32_t kg = 0, vg = 0;
+    uint4 ck[kPer] = {}, cv[kPer] = {};
     bool ok = true;
     Item x;
     for (int it = 0; ok && next_item(it, x); ++it) {
@@ -512,7 +577,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
       if (n <= 0) continue;
       const int32_t* table = A.table + x.b * A.ld_table;
       const int seen = min(min(x.before + (min(x.row0 + kPair, x.n_rows) - 1) / A.group + 1, A.max_kv), int(min((long long)A.table_width << A.shift, (long long)INT32_MAX)));
-      // This thread's pieces of 16 codes, copied and converted by itself.  Heads of 128 channels: eight neighbouring lanes take four
+      // This thread's pieces of 16 codes, read a step ahead into registers.  Heads of 128 channels: eight neighbouring lanes take four
       // pieces of two rows, whose places in the tile lie in different banks.
       auto row_at = [&](int i) { return kSteps == 8 ? i * 16 + ((t >> 4) << 1 | (t >> 2 & 1)) : (i * 128 + t) / kSteps; };
       auto piece_of = [&](int i) { return kSteps == 8 ? (t & 3) | (t >> 3 & 1) << 2 : (i * 128 + t) % kSteps; };
@@ -523,27 +588,29 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
         if (j < n && key < seen) asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(page) : "l"(table + (key >> A.shift)));
         return page;
       };
-      // in units of 16 bytes
-      const uint32_t block_units = uint32_t(A.c.kv_heads * kSteps) << A.shift, head_units = uint32_t(x.h * kSteps) << A.shift;
-      auto fetch = [&](uint8_t* raw, const uint8_t* codes, int page) {
-#pragma unroll 2
+      // Where a lane's group of 16 keys lies, in units of 16 bytes (no block: kNone; pieces then keep what they hold, their tokens weigh nothing)
+      constexpr uint32_t kNone = 0xffffffffu;
+      const uint32_t block_units = uint32_t(A.c.kv_heads * kSteps) << A.shift;
+      const uint32_t group_units = (uint32_t(x.h) << A.shift | uint32_t(16 * (lane & 7) & ((1 << A.shift) - 1))) * kSteps;          // (steps begin blocks)
+      // (volatile: a load that moved down to its use would be waited for there)
+      auto fetch = [&](uint4 (&c)[kPer], const uint8_t* codes, int page) {
+        const uint32_t group = unsigned(page) < unsigned(A.c.num_blocks) ? uint32_t(page) * block_units + group_units : kNone;
+#pragma unroll
         for (int i = 0; i < kPer; ++i) {
-          const int r = row_at(i), pg = __shfl_sync(0xffffffffu, page, r >> 4);
-          // (steps begin blocks; pieces of no block keep any bytes: their tokens weigh nothing)
-          if (unsigned(pg) < unsigned(A.c.num_blocks)) {
-            const uint32_t at = uint32_t(pg) * block_units + head_units + uint32_t((r & ((1 << A.shift) - 1)) * kSteps + piece_of(i));
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(raw) + uint32_t(i * 128 + t) * 16u), "l"(codes + uint64_t(at) * 16) : "memory");
-          }
+          const int r = row_at(i);
+          const uint32_t from = __shfl_sync(0xffffffffu, group, r >> 4);
+          asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0xffffffff;\n\t@p ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                       : "+r"(c[i].x), "+r"(c[i].y), "+r"(c[i].z), "+r"(c[i].w)
+                       : "l"(codes + uint64_t(from + uint32_t((r & 15) * kSteps + piece_of(i))) * 16), "r"(from) : "memory");
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
       };
-      auto convert = [&](const uint8_t* raw, uint8_t* tile, bool k) {
+      auto convert = [&](const uint4 (&raw)[kPer], uint8_t* tile, bool k) {
         auto lo = [&](uint32_t w) { return k ? bf16_codes(w, 0x4140) : codes_lo(w); };
         auto hi = [&](uint32_t w) { return k ? bf16_codes(w, 0x4342) : codes_hi(w); };
-#pragma unroll 2
+#pragma unroll
         for (int i = 0; i < kPer; ++i) {
           const int r = row_at(i), p = piece_of(i);
-          const uint4 c = *reinterpret_cast<const uint4*>(raw + (i * 128 + t) * 16);
+          const uint4 c = raw[i];
           *reinterpret_cast<uint4*>(tile + piece_at(r, 2 * p)) = make_uint4(lo(c.x), hi(c.x), lo(c.y), hi(c.y));
           *reinterpret_cast<uint4*>(tile + piece_at(r, 2 * p + 1)) = make_uint4(lo(c.z), hi(c.z), lo(c.w), hi(c.w));
         }
@@ -556,15 +623,14 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
 #pragma unroll 1
       for (int j = -1; j < n; ++j) {
         if (j >= 0) {
-          asm volatile("cp.async.wait_group 1;" ::: "memory");                 // (K of this step; its V may be on its way)
           if (!(ok = __all_sync(0xffffffffu, wait_for(S.k_empty[kg & 1], (kg >> 1) ^ 1u, abort, 108, P.status)))) break;
           if (t < 8) S.scale[kg & 3][t] = vs > 0.f ? make_float4(ks, lg2(vs), __fdividef(1.f, vs), 0.f) : make_float4(1.f, -CUDART_INF_F, 0.f, 0.f);
-          convert(S.raw[0], S.k[kg & 1], true);
+          convert(ck, S.k[kg & 1], true);
           if (lane == 0) mbar_arrive(smem_u32(&S.k_full[kg & 1]));
           ++kg;
         }
         const int now = page;
-        fetch(S.raw[0], A.c.k_codes, now);                // (past the last step: no blocks, nothing is copied)
+        fetch(ck, A.c.k_codes, now);                      // (past the last step: no blocks, nothing is read)
         if (t < 8) {
           vs = 0.f;
           if (unsigned(now) < unsigned(A.c.num_blocks)) {
@@ -575,15 +641,13 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
         }
         page = page_of(j + 2);
         if (j >= 0) {
-          asm volatile("cp.async.wait_group 1;" ::: "memory");                 // (V of this step; the next one's K may be on its way)
           if (!(ok = __all_sync(0xffffffffu, wait_for(S.v_empty[vg & 1], (vg >> 1) ^ 1u, abort, 109, P.status)))) break;
-          convert(S.raw[1], S.v[vg & 1], false);
+          convert(cv, S.v[vg & 1], false);
           if (lane == 0) mbar_arrive(smem_u32(&S.v_full[vg & 1]));
           ++vg;
         }
-        fetch(S.raw[1], A.c.v_codes, now);
+        fetch(cv, A.c.v_codes, now);
       }
-      asm volatile("cp.async.wait_all;" ::: "memory");
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
@@ -631,7 +695,13 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
       if (lane == 0) mbar_arrive(smem_u32(&S.q_full[i]));
     };
     bool ok = true;
-    bool more = see_item(0);
+    bool more = see_item(0), q_next = false;
+    // the next item's queries come while the last weights are formed
+    auto ask_next = [&](int it) {
+      more = see_item(it + 1);
+      q_next = more && S.item[(it + 1) & 1].ends[i] > 0;
+      if (q_next) ask_q(S.item[(it + 1) & 1]);
+    };
     if (more && S.item[0].ends[i] > 0) { ask_q(S.item[0]); give_q(); }
     for (int it = 0; more; ++it) {
       const volatile Item& x = S.item[it & 1];
@@ -648,6 +718,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
         if (!(ok = __all_sync(0xffffffffu, wait_for(S.s_full[i][half], ph_s >> half, abort, 110, P.status)))) break;
         ph_s ^= 1u << half;
         tc_fence_after();
+        if (u + 1 == n) ask_next(it);                     // (all products with this item's queries are done)
         const bool masked = __any_sync(0xffffffffu, sees < kHalf);
         const uint32_t t_u = t_s + 64u * half;
         float4 g[4];
@@ -722,16 +793,12 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
         ph_pv ^= 1u << half;                              // this step's product comes next
       }
       if (!ok) break;
-      // the next item's queries come while the last product and the output run (the S MMAs have read this one's)
-      more = see_item(it + 1);
-      const volatile Item& y = S.item[(it + 1) & 1];
-      const bool q_next = more && y.ends[i] > 0;
-      if (q_next) ask_q(y);
+      if (n == 0) ask_next(it);
+      if (q_next) give_q();
       if (n > 0) {
         ok = __all_sync(0xffffffffu, wait_for(S.pv_done[i][(n - 1) & 1], (ph_pv >> ((n - 1) & 1)) ^ 1u, abort, 112, P.status));
         tc_fence_after();
       }
-      if (q_next) give_q();
       if (!ok) break;
       kg += uint32_t((max(x.ends[0], x.ends[1]) + 1) >> 1);
       const OutRow row = row_of(x);
@@ -752,9 +819,15 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
         if (writes) __threadfence();
       }
       if (writes) {
-        const float2 mz = put_row<kSteps>(A, row, r, i, t_o, n > 0, m, z, w0, parts);
+        if (parts > 1) {
+          const float2 mz = join_parts<kSteps>(A, r, i, t_o, w0, parts);
+          m = mz.x;
+          z = mz.y;
+        }
+        const float inv = z > 0.f ? __fdividef(1.f, z) : z == 0.f ? 0.f : CUDART_NAN_F;
+        put_rows<kSteps>(A, S.stage[warp], row.in ? row.token * A.ldo + row.head * A.o_sh : -1, row.token, t_o, n > 0 || parts > 1, inv, lane);
         if (row.in && A.lse)
-          A.lse[int64_t(row.token) * A.heads + row.head] = mz.y > 0.f ? (mz.x - kLift + log2f(mz.y)) * kLn2 : mz.y == 0.f ? -CUDART_INF_F : CUDART_NAN_F;
+          A.lse[int64_t(row.token) * A.heads + row.head] = z > 0.f ? (m - kLift + log2f(z)) * kLn2 : z == 0.f ? -CUDART_INF_F : CUDART_NAN_F;
       }
       if (n > 0) {
         tc_fence_before();
