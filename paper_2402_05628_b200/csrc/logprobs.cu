@@ -348,17 +348,16 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const __grid_c
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) least = fmaxf(least, warp_most[w]);
     } else {
-      if (warp == kWarps - 1) {                    // the K-th largest of the 64
-        const float a = group_top[lane], b = group_top[lane + 32];
-        int na = 0, nb = 0;                        // groups ahead of mine, ties by place
+      if (tid >= kThreads - 64) {                  // the K-th largest of the 64
+        const int mine = tid - (kThreads - 64);
+        const float a = group_top[mine];
+        int n = 0;                                 // groups ahead of mine, ties by place
 #pragma unroll 8
         for (int i = 0; i < 64; ++i) {
           const float x = group_top[i];
-          na += x > a || (x == a && i < lane) ? 1 : 0;
-          nb += x > b || (x == b && i < lane + 32) ? 1 : 0;
+          n += x > a || (x == a && i < mine) ? 1 : 0;
         }
-        if (na == P.top - 1) bound = a;
-        if (nb == P.top - 1) bound = b;
+        if (n == P.top - 1) bound = a;
       }
       __syncthreads();
       least = bound;
@@ -452,11 +451,17 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const __grid_c
       for (int i = tid; i < kSplit * P.top; i += kThreads) {
         const int ip = i / P.top, ik = i - ip * P.top;
         const uint64_t key = all_top[ip][ik];
-        int before = ik;                           // a part's own are in order
-#pragma unroll 1
-        for (int p = 0; p < kSplit; ++p)
-          if (p != ip)
-            for (int k = 0; k < P.top && (all_top[p][k] > key || (all_top[p][k] == key && p < ip)); ++k) ++before;
+        int before = ik;                           // a part's own are in order; of another's, bisection counts those ahead
+#pragma unroll
+        for (int p = 0; p < kSplit; ++p) {
+          int n = 0;
+#pragma unroll
+          for (int step = kMostTop; step > 0; step >>= 1) {
+            const uint64_t other = n + step <= P.top ? all_top[p][n + step - 1] : 0;
+            if (n + step <= P.top && (other > key || (other == key && p < ip))) n += step;
+          }
+          before += p != ip ? n : 0;
+        }
         if (before < P.top) put(before, key);
       }
     }
