@@ -52,9 +52,11 @@ repq_status prepare(const repq_cache_attention_desc* d, AttendParams* out, bool*
 bool nothing(const AttendParams& P) { return P.requests == 0 || P.max_q == 0; }
 
 // Which kernels a call takes.  Requests of up to kFewRows rows go to the kernel for few rows, others to the one for chunks; float32
-// queries always to the former.  Lengths are known on the device only: where the bounds allow both kinds both kernels run, each passes
-// over the other's requests.
-constexpr int kFewRows = 48;
+// queries always to the former.  (Few rows / chunks, 8 heads over 32 x 4096, 4 x 4096 and 64 x 600 tokens: 128 channels, 24 rows 146 / 154, 36 / 47 and
+// 69 / 87 us; 40 rows 223 / 147, 42 / 45 and 100 / 84; 64 channels, 40 rows 121 / 135, 33 / 36 and 63 / 68; 48 rows 165 / 137, 36 / 37 and
+// 77 / 68.  The kernel for few rows keeps more bits of small weights.)  Lengths are known on the device only: where the bounds allow both kinds both
+// kernels run, each passes over the other's requests.
+constexpr int kFewRows = 40;
 struct Route { bool rows, chunks; int few; RowsPlan rp; ChunksPlan cp; size_t rows_bytes, workspace; };
 repq_status route_of(AttendParams& P, bool precise, Route* out) {
   Route r = {};
