@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const __grid_c
 // maxima in shared memory.  Either way every row is read once, all its loads in flight together (a run per warp whatever its length, read
 // twice where it did not fit: 75 us for 2400 tokens of 32 heads of 128 channels in blocks of 64; floor 9).
 constexpr int kHeld = 8;                          // pieces of eight elements that a thread holds
-constexpr int kMostWindow = 128;
+constexpr int kMostWindow = 64;
 
 struct WriteParams {
   repq_cache c;
@@ -400,7 +400,8 @@ extern "C" repq_status repq_cache_write(const repq_cache_write_desc* d, void* st
   P.shift = cache::log2_block(d->cache.block_size);
   P.pieces = d->cache.d_h / 8;
   P.by_pieces = (65536 + P.pieces - 1) / P.pieces;
-  // windows such that there are some sixteen CTAs per SM; four tokens where there are few (a warp each)
+  // windows such that there are some sixteen CTAs per SM, of 64 tokens at most (2400 tokens of 32 heads: 33 us with windows of 64, 36 with 128,
+  // 51 with 4); four tokens where there are few (a warp each; 64 single tokens of 32 heads 11 us, 31 with one window)
   const int64_t per = int64_t(d->tokens) * d->cache.kv_heads / (int64_t(sm_count()) * 8);
   P.window = 4;
   while (P.window < per && P.window < cache::kMostWindow) P.window *= 2;
