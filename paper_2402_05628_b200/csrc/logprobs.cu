@@ -231,6 +231,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const __grid_c
   // and what the third has (so that a thread hardly ever has to look at all of its vectors again: 106 -> 88 us for 5 of 4096 x 32000).
   float best = -CUDART_INF_F, second = -CUDART_INF_F, third = -CUDART_INF_F;
   int best_e = begin, second_e = begin;
+  float limit = -CUDART_INF_F, minus = 0.f;        // above limit m moves; -m (0 as long as m is below -1e38: what is not above limit is -inf then)
   f32x2 z2 = splat2(0.f), w2 = splat2(0.f);        // sums of the pairs' halves since m last moved
   auto settle = [&]() {
     float a, b;
@@ -250,47 +251,57 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const __grid_c
       second = fmaxf(second, fminf(top, best));
     }
     if (top > best) { best = top; best_e = e; }
-    if (top > s.m + kLag) { settle(); move_to(s, top); }
-    if (s.m > -1e38f) {
-      float f[kN];
-      Vec<T>::get(Vec<T>::floored(v), f);          // (0 * -inf would be a NaN)
-      const f32x2 mm = splat2(-s.m), c = splat2(kLog2e);
-#pragma unroll
-      for (int i = 0; i < kN / 2; ++i) {
-        const f32x2 d = add2(pack2(f[2 * i], f[2 * i + 1]), mm);
-        float a, b;
-        unpack2(mul2(d, c), a, b);
-        const f32x2 p = pack2(ex2(a), ex2(b));
-        z2 = add2(z2, p);
-        w2 = fma2(p, d, w2);
-      }
-    } else {
-      const float2 zw = careful_sums<T>(v, s.m == -CUDART_INF_F ? 0.f : s.m);
-      s.z += zw.x;
-      s.w += zw.y;
-    }
     // what comes before the given token: larger ones, in front of it equal ones too
     // (few vectors have any where the token is a plausible one)
     const float over = e < token ? xb : xt;
     if (top > over) ahead2 += Vec<T>::above(v, over);
+    if (top > limit) {
+      if (top > s.m + kLag) { settle(); move_to(s, top); }
+      if (!(s.m > -1e38f)) {
+        const float2 zw = careful_sums<T>(v, s.m);
+        s.z += zw.x;
+        s.w += zw.y;
+        return;
+      }
+      limit = s.m + kLag;
+      minus = -s.m;
+    }
+    float f[kN];
+    Vec<T>::get(Vec<T>::floored(v), f);            // (0 * -inf would be a NaN)
+    const f32x2 mm = splat2(minus), c = splat2(kLog2e);
+#pragma unroll
+    for (int i = 0; i < kN / 2; ++i) {
+      const f32x2 d = add2(pack2(f[2 * i], f[2 * i + 1]), mm);
+      float a, b;
+      unpack2(mul2(d, c), a, b);
+      const f32x2 p = pack2(ex2(a), ex2(b));
+      z2 = add2(z2, p);
+      w2 = fma2(p, d, w2);
+    }
   };
   const int step = kThreads * kN;
   int since = 0;
+  int e = begin + tid * kN;
 #pragma unroll 1
-  for (int e = begin + tid * kN; e < end; e += kFly * step) {
+  for (; e + (kFly - 1) * step < end; e += kFly * step) {
     uint4 v[kFly];
 #pragma unroll
-    for (int i = 0; i < kFly; ++i)
-      if (e + i * step < end) v[i] = load_vec<T, kWhole>(P, row, e + i * step, end);
+    for (int i = 0; i < kFly; ++i) v[i] = load_vec<T, kWhole>(P, row, e + i * step, end);
 #pragma unroll
-    for (int i = 0; i < kFly; ++i)
-      if (e + i * step < end) take(v[i], e + i * step);
+    for (int i = 0; i < kFly; ++i) take(v[i], e + i * step);
     if (++since == 4000 / kFly) {                  // (a half of the count takes four of a vector)
       ahead += Vec<T>::kLow ? int(ahead2 & 0xffffu) + int(ahead2 >> 16) : int(ahead2);
       ahead2 = 0u;
       since = 0;
     }
   }
+  uint4 v[kFly - 1];                               // what is left
+#pragma unroll
+  for (int i = 0; i < kFly - 1; ++i)
+    if (e + i * step < end) v[i] = load_vec<T, kWhole>(P, row, e + i * step, end);
+#pragma unroll
+  for (int i = 0; i < kFly - 1; ++i)
+    if (e + i * step < end) take(v[i], e + i * step);
   ahead += Vec<T>::kLow ? int(ahead2 & 0xffffu) + int(ahead2 >> 16) : int(ahead2);
   if (given && begin <= token && token < end && tid == (token - begin) / kN % kThreads) {
     // in the given token's own vector: it and its equals behind it have been counted, unless the vector begins with it
