@@ -483,9 +483,8 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const __grid_c
   }
 }
 
-template <typename T, int kSplit, bool kMany>
+template <typename T, int kThreads, int kSplit, bool kMany>
 repq_status launch_form(const Params& P, cudaStream_t st) {
-  constexpr int kThreads = kSplit == 1 ? 128 : 256;      // (what a row costs beside its elements is per warp)
   const bool whole = P.vec && P.vocab % Vec<T>::kN == 0;
   const dim3 grid(unsigned(P.rows) * kSplit), block(kThreads);
   if (whole) REPQ_CUDA(launch_chained_cluster(token_logprobs_kernel<T, kThreads, kSplit, true, kMany>, grid, block, 0, st, kSplit, P));
@@ -493,9 +492,9 @@ repq_status launch_form(const Params& P, cudaStream_t st) {
   note_launch();
   return REPQ_OK;
 }
-template <typename T, int kSplit>
+template <typename T, int kThreads, int kSplit>
 repq_status launch(const Params& P, cudaStream_t st) {
-  return P.top > 1 ? launch_form<T, kSplit, true>(P, st) : launch_form<T, kSplit, false>(P, st);
+  return P.top > 1 ? launch_form<T, kThreads, kSplit, true>(P, st) : launch_form<T, kThreads, kSplit, false>(P, st);
 }
 
 template <typename T>
@@ -506,10 +505,12 @@ repq_status choose(Params& P, cudaStream_t st) {
   while (split < kMostSplit && P.rows * split * 2 <= 4 * sm_count() && P.vocab / (split * 2) >= 1024) split *= 2;
   P.per = int(round_up((P.vocab + split - 1) / split, 8));
   switch (split) {
-    case 1: return launch<T, 1>(P, st);
-    case 2: return launch<T, 2>(P, st);
-    case 4: return launch<T, 4>(P, st);
-    default: return launch<T, 8>(P, st);
+    // (What a row costs beside its elements is per warp, so four warps where rows fill the SMs so too: 4096 rows of 32000 72 us, 80 with eight warps;
+    // 512 rows 22 and 20, 1024 rows of 128000 98 and 81.)
+    case 1: return P.rows > 8 * sm_count() ? launch<T, 128, 1>(P, st) : launch<T, 256, 1>(P, st);
+    case 2: return launch<T, 256, 2>(P, st);
+    case 4: return launch<T, 256, 4>(P, st);
+    default: return launch<T, 256, 8>(P, st);
   }
 }
 

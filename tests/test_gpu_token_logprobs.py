@@ -109,6 +109,33 @@ def test_token_logprobs_ties_masks_and_padding(B, rows):
     check(B, torch.from_numpy(y), tokens, 3)
 
 
+@pytest.mark.parametrize("act", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows,vocab,top", [(1300, 600, 6), (1250, 1501, 1), (1201, 515, 0), (1300, 2048, 32)])
+def test_token_logprobs_many_rows(B, rows, vocab, top, act):
+    """Enough rows that each has few warps."""
+    import torch
+    rng = np.random.default_rng(vocab + top)
+    x = (2 * rng.standard_normal((rows, vocab))).astype(np.float32)
+    x[::7, rng.integers(0, vocab, vocab // 2)] = -np.inf
+    x[3::11] = np.round(x[3::11])                                  # (many equal ones)
+    tokens = rng.integers(0, vocab, rows)
+    tokens[::5] = -1
+    check(B, torch.from_numpy(x).to(getattr(torch, act)), tokens, top)
+
+
+@pytest.mark.parametrize("act", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows", [1, 320, 1200])
+def test_token_logprobs_largest_far_apart(B, rows, act):
+    """The largest logits lie at a power of two of elements from each other, so that they fall to few threads, or to one."""
+    import torch
+    rng = np.random.default_rng(rows)
+    x = rng.standard_normal((rows, 8192)).astype(np.float32)
+    for r in range(rows):
+        step = (512, 1024, 2048)[r % 3]
+        x[r, r % 16::step] += 20.0
+    check(B, torch.from_numpy(x).to(getattr(torch, act)), rng.integers(0, 8192, rows), 12)
+
+
 @pytest.mark.parametrize("rows", [5, 500])
 def test_token_logprobs_rows_of_nothing_nan_and_infinity(B, rows):
     import torch
