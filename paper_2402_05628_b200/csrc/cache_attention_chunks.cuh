@@ -49,11 +49,14 @@ constexpr float kLn2 = 0.6931471805599453f;
 // there; w0, parts: the first of the CTAs that share it, and their number
 struct Item { int b, h, row0, q0, before, n_rows, j0, ends[2], w0, parts; };
 constexpr int kItemCost = 2;             // steps
-constexpr int kLeastShare = 4;           // positions of a CTA
+// Positions of a CTA at least: 4 (a request of 256 tokens, 32 heads: 20 us; 33 with 6, 29 with 8), and the root of half of what the longest item may have, since
+// joining a part takes half as long as a step (128 queries of 8 heads over 8192 tokens: 49 us with 6, 61 with 4).
+constexpr int kLeastShare = 4;
 
 struct ChunkParams {
   AttendParams a;
   int few;                               // requests of at most this many rows are not this kernel's
+  int least;                             // positions of a CTA
   int32_t* status;
 };
 
@@ -136,7 +139,7 @@ __device__ __forceinline__ long long length_of(const ChunkParams& P, const Reque
   for (int i = pairs_of(P, rq); i > 0; --i) n += (long long)(steps_of(P, rq, i - 1) + kItemCost) * P.a.c.kv_heads;
   return n;
 }
-__device__ __forceinline__ long long workers_of(long long total) { return max(min((long long)gridDim.x, total / kLeastShare), total > 0 ? 1ll : 0ll); }
+__device__ __forceinline__ long long workers_of(const ChunkParams& P, long long total) { return max(min((long long)gridDim.x, total / P.least), total > 0 ? 1ll : 0ll); }
 
 // place of 16-byte piece `c` (eight channels) of row `r` in a swizzled tile
 __device__ __forceinline__ uint32_t piece_at(int r, int c) {
@@ -384,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
       total += S.sums[w];
     }
     // the group of requests that the share begins in
-    const long long workers = workers_of(total), at = blockIdx.x < workers ? blockIdx.x * total / workers : total;
+    const long long workers = workers_of(P, total), at = blockIdx.x < workers ? blockIdx.x * total / workers : total;
     if (before - n <= at && at < before) { S.request = b_first; S.from = before - n; }
     if (tid == 0) {
       S.total = total;
@@ -408,7 +411,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_chunks_kernel(const __grid_
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == kItemWarp) {
       // ---------------------------------------------------------------- items (every lane walks the line alike)
-      const long long total = S.total, workers = workers_of(total);
+      const long long total = S.total, workers = workers_of(P, total);
       const bool any = blockIdx.x < workers;
       long long at = S.share[0], start = any ? S.from : 0;
       const long long begin = at, end = S.share[1];
@@ -865,6 +868,8 @@ repq_status launch(const AttendParams& A, const ChunksPlan& plan, int few, void*
   ChunkParams P;
   P.a = A;
   P.few = few;
+  P.least = kLeastShare;
+  while (2 * P.least * P.least < A.max_kv / kKeys) ++P.least;
   P.a.counters = static_cast<int32_t*>(workspace);
   P.a.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + plan.counter_bytes);
   P.status = device_status_word();
