@@ -14,7 +14,7 @@
 //
 // With x = S alpha k_scale log2 e, a row keeps m, the largest x + log2 v_scale seen, Z = sum 2^(x - m + 15) and
 // O = sum 2^(x - m + 15) v_scale (c - 128): weights of the second product lie in f16's range whatever the blocks' scales are, with
-// 11 bits down to 2^-29 of the largest (float32 queries: queries and weights as two f16 numbers each, 22 bits).
+// 11 bits down to 2^-29 of the largest (float32 queries: queries and weights as two f16 numbers each, 22 bits; errors 5e-7 where long sums inside the tensor cores had 2.1e-6).
 //
 // 64 requests of 1 to 4096 tokens, 32 heads of 128 channels on 8: 53 us (83 at first), their bytes take 40; 2 requests of 131072: 99 (113), 83.  What is
 // left: the conversions' instructions (issue slots busy 49 to 52 %) beside loads that registers hold only 16 keys ahead a warp.  Keys through a ring in
@@ -35,6 +35,13 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// d = the product alone.  The tensor cores' additions cut off bits, always towards zero, so that a long chain of them shrinks what it sums (by 2e-6 of it
+// over 4091 keys); float32 queries add products of their own to sums with rounded additions.
+__device__ __forceinline__ void mma_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   uint32_t y;
@@ -187,8 +194,15 @@ struct Rows {
       const uint32_t a[4] = {codes_lo(K.k[0][j]), codes_lo(K.k[1][j]), codes_hi(K.k[0][j]), codes_hi(K.k[1][j])};
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) {
-        mma(j & 1 ? s2[i] : s[i], a, q[i][2 * j], q[i][2 * j + 1]);
-        if constexpr (kPrecise) mma(j & 1 ? s[i] : s2[i], a, ql[i][2 * j], ql[i][2 * j + 1]);
+        if constexpr (kPrecise) {                  // (s2: the queries' low halves)
+          float x[4];
+          mma_first(x, a, q[i][2 * j], q[i][2 * j + 1]);
+          mma(s2[i], a, ql[i][2 * j], ql[i][2 * j + 1]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[i][e] += x[e];
+        } else {
+          mma(j & 1 ? s2[i] : s[i], a, q[i][2 * j], q[i][2 * j + 1]);
+        }
       }
     }
 #pragma unroll
@@ -261,8 +275,15 @@ struct Rows {
           const uint32_t a[4] = {codes_lo(x), codes_hi(x), codes_lo(y), codes_hi(y)};
 #pragma unroll
           for (int i = 0; i < kTiles; ++i) {
-            mma(o[i][j + u], a, p[i][0], p[i][1]);
-            if constexpr (kPrecise) mma(o[i][j + u], a, pl[i][0], pl[i][1]);
+            if constexpr (kPrecise) {
+              float x[4];
+              mma_first(x, a, pl[i][0], pl[i][1]);
+              mma(x, a, p[i][0], p[i][1]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[i][j + u][e] += x[e];
+            } else {
+              mma(o[i][j + u], a, p[i][0], p[i][1]);
+            }
           }
         }
       }
