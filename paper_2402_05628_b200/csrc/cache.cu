@@ -149,8 +149,8 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const __grid_c
 // of consecutive slots in one block).  A CTA takes a window of tokens and K or V of one head; the window's runs are found by a vote.  A run that
 // fits a warp's registers (16 rows of 128 channels) is a warp's; a longer one is shared by the CTA's warps, which join their
 // maxima in shared memory.  Either way every row is read once, all its loads in flight together (a run per warp whatever its length, read
-// twice where it did not fit: 75 us for 2400 tokens of 32 heads of 128 channels in blocks of 64, 33 now).  The bytes of that take 9 us at the memory's
-// rate; what bounds it now is 19 instructions an element (issue slots busy 48 %) and the latency of slot map, scale and rows one after the other.
+// twice where it did not fit: 75 us for 2400 tokens of 32 heads of 128 channels in blocks of 64, 33 now, 26 back to back).  The bytes of that take 9 us at the memory's
+// rate; what bounds it now is 20 instructions an element (issue slots busy 54 %) and the latency of slot map, scale and rows one after the other.
 constexpr int kHeld = 8;                          // pieces of eight elements that a thread holds
 constexpr int kMostWindow = 64;
 
