@@ -345,6 +345,11 @@ def test_attention_chunks(B, kv, q, heads, kv_heads, dh, bs):
     Case(kv, q, heads, kv_heads, dh, bs, seed=sum(q)).check(B)
 
 
+@pytest.mark.parametrize("kv,q,heads,kv_heads,dh,bs", [([9000], [64], 2, 2, 64, 32), ([20000, 300], [50, 44], 2, 1, 128, 64)])
+def test_attention_chunks_of_long_items_in_few_parts(B, kv, q, heads, kv_heads, dh, bs):
+    Case(kv, q, heads, kv_heads, dh, bs, seed=sum(kv)).check(B)
+
+
 def test_attention_chunks_rising_maxima(B):
     """Keys that matter more the later they come, by far: the running maximum moves within steps and between them."""
     c = Case([600], [200], 2, 2, 64, 32, seed=21)
